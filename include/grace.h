@@ -23,6 +23,8 @@
  *   grace_gtm_mask        decode-time constraint filter: constrained decoding on
  *                         the SID trie and target matching (Sec. 4, Sec. 5.4, App. A);
  *   grace_trie_advance    the trie node each selected beam moves to (Sec. 4.4);
+ *   grace_rms_norm        norm of the residual stream, with the residual's addition
+ *                         and, if wanted, an output in 8 bits;
  *   grace_graph_*         capture of a sequence of these calls (a whole decode
  *                         loop) as one replayable HIP graph (Sec. 5).
  *
@@ -60,7 +62,9 @@
 extern "C" {
 #endif
 
-enum grace_dtype { GRACE_F32 = 0, GRACE_BF16 = 1 };
+/* GRACE_E4M3 (OCP 8-bit float, 4 exponent and 3 mantissa bits, largest 448) is
+ * taken by grace_rms_norm (output) and grace_linear (inputs) only. */
+enum grace_dtype { GRACE_F32 = 0, GRACE_BF16 = 1, GRACE_E4M3 = 2 };
 
 enum grace_status {
   GRACE_OK = 0,
@@ -429,6 +433,42 @@ int32_t grace_trie_advance(const grace_gtm_index* index, const int32_t* node_pre
                            const int32_t* parents, const int32_t* tokens, int32_t B,
                            int32_t M_prev, int32_t k, int32_t* node_next, int32_t* err_flag,
                            void* stream);
+
+/* Longest row grace_rms_norm accepts (32768). */
+int32_t grace_rms_norm_max_d(void);
+
+/*
+ * Root-mean-square norm of the residual stream, between two sublayers of a
+ * decode step.  For every row r:
+ *   h   = x[r] + residual[r]                     (h = x[r] without a residual)
+ *   sum[r] = h
+ *   y   = h / sqrt(mean(h^2) + eps) * weight
+ *   out[r] = y                                   (out_dtype GRACE_F32 or GRACE_BF16)
+ *   out_scale[r] = max(max|y|, 2^-96) / 448,     (out_dtype GRACE_E4M3)
+ *   out[r] = y / out_scale[r]
+ * in fp32 (the norm takes h before its rounding to sum); each output is rounded
+ * to nearest-even once.  out_scale[r] * out[r] stands for y.  A row that holds a
+ * NaN or an infinity, or whose squares pass the range of fp32, has no defined
+ * norm; the other rows are not touched by it.
+ *
+ *   x          device, [R, D], dtype
+ *   residual   device, [R, D], dtype, or NULL
+ *   weight     device, [D], dtype
+ *   R, D       rows and row length; R >= 0 (0 is a no-op),
+ *              1 <= D <= grace_rms_norm_max_d()
+ *   eps        finite and > 0
+ *   dtype      GRACE_F32 or GRACE_BF16 (x, residual, weight, sum)
+ *   out_dtype  GRACE_F32, GRACE_BF16 or GRACE_E4M3
+ *   sum        device, [R, D], dtype, or NULL; may be x or residual itself (the
+ *              stream updated in place)
+ *   out        device, [R, D], out_dtype
+ *   out_scale  device, fp32 [R]; required for GRACE_E4M3, else not used
+ *   stream     hipStream_t
+ * Apart from sum in place, no written range may overlap another or a read one.
+ */
+int32_t grace_rms_norm(const void* x, const void* residual, const void* weight, int32_t R,
+                       int32_t D, float eps, int32_t dtype, int32_t out_dtype, void* sum,
+                       void* out, float* out_scale, void* stream);
 
 /*
  * Graph capture (Sec. 5: the fixed-length decoding loop is captured as one

@@ -41,6 +41,12 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, b);
 }
 
+// Four fp32 -> four e4m3 (OCP, largest 448) in one word, round to nearest even.
+__device__ __forceinline__ uint32_t pack_e4m3x4(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
 // A 16-byte chunk as fp32 lanes: 4 floats or 8 bf16.
 template <class T> struct Chunk;
 template <> struct Chunk<F32> {

@@ -16,7 +16,9 @@ thread_local int32_t g_last_hip_error = 0;
 
 bool supported_d(int32_t d) { return d == 32 || d == 64 || d == 128; }
 
-int32_t elem_bytes(int32_t dtype) { return dtype == GRACE_F32 ? 4 : 2; }
+int32_t elem_bytes(int32_t dtype) {
+  return dtype == GRACE_F32 ? 4 : (dtype == GRACE_BF16 ? 2 : 1);
+}
 
 // Byte ranges [a, a+na) and [b, b+nb) overlap.
 bool overlaps(const void* a, int64_t na, const void* b, int64_t nb) {
@@ -476,6 +478,45 @@ int32_t grace_trie_advance(const grace_gtm_index* index, const int32_t* node_pre
     if (overlaps(node_next, n, r.p, r.n)) return GRACE_ERR_ALIAS;
   return hip_status(grace::launch_trie_advance(*index, node_prev, parents, tokens, B, M_prev, k,
                                                node_next, err_flag, (hipStream_t)stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+bool good_dtype(int32_t dtype) { return dtype >= GRACE_F32 && dtype <= GRACE_E4M3; }
+
+}  // namespace
+
+extern "C" {
+
+int32_t grace_rms_norm_max_d(void) { return grace::rms_norm_max_d(); }
+
+int32_t grace_rms_norm(const void* x, const void* residual, const void* weight, int32_t R,
+                       int32_t D, float eps, int32_t dtype, int32_t out_dtype, void* sum,
+                       void* out, float* out_scale, void* stream) {
+  if ((dtype != GRACE_F32 && dtype != GRACE_BF16) || !good_dtype(out_dtype))
+    return GRACE_ERR_UNSUPPORTED;
+  if (R < 0 || D < 1 || D > grace::rms_norm_max_d()) return GRACE_ERR_SHAPE;
+  if (!isfinite(eps) || eps <= 0.f) return GRACE_ERR_SHAPE;
+  if (R == 0) return GRACE_OK;
+  if (!x || !weight || !out || (out_dtype == GRACE_E4M3 && !out_scale)) return GRACE_ERR_NULL;
+  const int64_t in_row = (int64_t)D * elem_bytes(dtype), n = R * in_row;
+  const Range reads[3] = {{x, n}, {residual, residual ? n : 0}, {weight, in_row}};
+  const Range writes[3] = {{out, (int64_t)R * D * elem_bytes(out_dtype)},
+                           {sum, sum ? n : 0},
+                           {out_scale, out_dtype == GRACE_E4M3 ? (int64_t)R * 4 : 0}};
+  for (int i = 0; i < 3; ++i) {
+    for (int j = i + 1; j < 3; ++j)
+      if (overlaps(writes[i].p, writes[i].n, writes[j].p, writes[j].n)) return GRACE_ERR_ALIAS;
+    for (int j = 0; j < 3; ++j) {
+      // the residual stream may be updated in place
+      if (i == 1 && j < 2 && sum == reads[j].p) continue;
+      if (overlaps(writes[i].p, writes[i].n, reads[j].p, reads[j].n)) return GRACE_ERR_ALIAS;
+    }
+  }
+  return hip_status(grace::launch_rms_norm(x, residual, weight, R, D, eps, dtype, out_dtype, sum,
+                                           out, out_scale, (hipStream_t)stream));
 }
 
 }  // extern "C"

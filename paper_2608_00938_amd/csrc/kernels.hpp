@@ -67,6 +67,14 @@ hipError_t launch_trie_advance(const grace_gtm_index& index, const int32_t* node
                                int32_t M_prev, int32_t k, int32_t* node_next, int32_t* err_flag,
                                hipStream_t stream);
 
+// Norm of R rows of D elements (D <= rms_norm_max_d()): h = x + residual (residual
+// may be null), sum = h if not null, out = h / rms(h) * weight in out_dtype, with
+// a scale per row for GRACE_E4M3.
+hipError_t launch_rms_norm(const void* x, const void* residual, const void* weight, int32_t R,
+                           int32_t D, float eps, int32_t dtype, int32_t out_dtype, void* sum,
+                           void* out, float* out_scale, hipStream_t stream);
+int32_t rms_norm_max_d();
+
 // Debug builds: add the device-check counters of the attention kernels' source
 // files to acc[0 .. 7] and clear them (synchronous); release builds return
 // hipErrorNotSupported.

@@ -17,10 +17,13 @@ import torch
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libgrace.so")
 _lib = None
 
-GRACE_F32, GRACE_BF16 = 0, 1
+GRACE_F32, GRACE_BF16, GRACE_E4M3 = 0, 1, 2
 GRACE_OK, GRACE_ERR_NULL, GRACE_ERR_SHAPE, GRACE_ERR_UNSUPPORTED, GRACE_ERR_ALIAS, GRACE_ERR_HIP = range(6)
 
 _DTYPE_CODE = {torch.float32: GRACE_F32, torch.bfloat16: GRACE_BF16}
+
+# types of the position-wise operators' outputs and 8-bit inputs
+_ANY_DTYPE_CODE = {**_DTYPE_CODE, torch.float8_e4m3fn: GRACE_E4M3}
 
 _c_int, _c_float, _c_void_p = ctypes.c_int32, ctypes.c_float, ctypes.c_void_p
 
@@ -73,6 +76,9 @@ _SIGNATURES = {
                        _c_int, _c_void_p, _c_void_p, _c_void_p],
     "grace_trie_advance": [ctypes.POINTER(GtmIndexC), _c_void_p, _c_void_p, _c_void_p, _c_int,
                            _c_int, _c_int, _c_void_p, _c_void_p, _c_void_p],
+    "grace_rms_norm_max_d": [],
+    "grace_rms_norm": [_c_void_p, _c_void_p, _c_void_p, _c_int, _c_int, _c_float, _c_int, _c_int,
+                       _c_void_p, _c_void_p, _c_void_p, _c_void_p],
     "grace_graph_begin": [_c_void_p],
     "grace_graph_end": [_c_void_p, ctypes.POINTER(_c_void_p)],
     "grace_graph_launch": [_c_void_p, _c_void_p],
@@ -428,6 +434,65 @@ def grace_trie_advance(index: GtmIndex, node_prev, parents, tokens, B: int, M_pr
                                       _stream(node_prev))
     _check(st, "grace_trie_advance")
     return node_next
+
+
+def _expect(name: str, t, shape, dtype, device):
+    """t is a contiguous tensor of this shape, type and device (or None): a call
+    that passes sizes and raw pointers has no other check of them."""
+    if t is None:
+        return
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, not {dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not {device}")
+    if not t.is_contiguous():
+        raise ValueError("tensors passed to libgrace must be contiguous")
+
+
+def _call(fn: str, like: torch.Tensor, *args):
+    """Call an entry point on the current stream of ``like``'s GPU, with that GPU
+    current (a kernel is launched on the current GPU)."""
+    stream = _stream(like)
+    if like.get_device() == torch.cuda.current_device():
+        _check(getattr(library(), fn)(*args, stream), fn)
+    else:
+        with torch.cuda.device(like.device):
+            _check(getattr(library(), fn)(*args, stream), fn)
+
+
+def grace_rms_norm_max_d() -> int:
+    return library().grace_rms_norm_max_d()
+
+
+def grace_rms_norm(x, weight, eps: float = 1e-6, residual=None, sum_out=None, out=None,
+                   out_dtype=None, out_scale=None):
+    """h = x + residual, out = h / sqrt(mean(h^2) + eps) * weight over the last
+    dimension; x [R, D] (fp32 or bf16), weight [D] of x's dtype.  ``sum_out``
+    receives h (it may be x or residual itself).  ``out_dtype``: out's dtype if
+    given, else x's; float32, bfloat16 or float8_e4m3fn.  Returns out, or
+    (out, out_scale fp32 [R]) in 8 bits: out * out_scale[:, None] stands for the norm."""
+    R, D = x.shape
+    dev, dtype = x.device, x.dtype
+    if out_dtype is None:
+        out_dtype = dtype if out is None else out.dtype
+    code, out_code = _dtype_code(x), _ANY_DTYPE_CODE.get(out_dtype)
+    if out_code is None:
+        raise TypeError(f"unsupported dtype {out_dtype}")
+    if out is None:
+        out = torch.empty(x.shape, dtype=out_dtype, device=dev)
+    if out_code == GRACE_E4M3 and out_scale is None:
+        out_scale = torch.empty((R,), dtype=torch.float32, device=dev)
+    _expect("x", x, x.shape, dtype, dev)
+    _expect("weight", weight, (D,), dtype, dev)
+    _expect("residual", residual, x.shape, dtype, dev)
+    _expect("sum_out", sum_out, x.shape, dtype, dev)
+    _expect("out", out, x.shape, out_dtype, dev)
+    _expect("out_scale", out_scale, (R,), torch.float32, dev)
+    _call("grace_rms_norm", x, _ptr(x), _ptr(residual), _ptr(weight), R, D, eps, code, out_code,
+          _ptr(sum_out), _ptr(out), _ptr(out_scale))
+    return (out, out_scale) if out_code == GRACE_E4M3 else out
 
 
 class Graph:
