@@ -25,6 +25,8 @@
  *   grace_trie_advance    the trie node each selected beam moves to (Sec. 4.4);
  *   grace_rms_norm        norm of the residual stream, with the residual's addition
  *                         and, if wanted, an output in 8 bits;
+ *   grace_linear          matrix product (projections, feed-forward, logits) with
+ *                         scales, bias, activation and residual in its epilogue;
  *   grace_graph_*         capture of a sequence of these calls (a whole decode
  *                         loop) as one replayable HIP graph (Sec. 5).
  *
@@ -469,6 +471,47 @@ int32_t grace_rms_norm_max_d(void);
 int32_t grace_rms_norm(const void* x, const void* residual, const void* weight, int32_t R,
                        int32_t D, float eps, int32_t dtype, int32_t out_dtype, void* sum,
                        void* out, float* out_scale, void* stream);
+
+/* Activations of grace_linear. */
+enum grace_act {
+  GRACE_ACT_NONE = 0,
+  GRACE_ACT_RELU = 1,   /* max(y, 0)                       */
+  GRACE_ACT_GELU = 2,   /* y (1 + erf(y / sqrt(2))) / 2    */
+  GRACE_ACT_SILU = 3    /* y / (1 + exp(-y))               */
+};
+
+/*
+ * Matrix product of the beam rows with a weight matrix, and its epilogue
+ * (projections around the attention, the feed-forward's two products, logits):
+ *   y           = x_scale[r] * w_scale[n] * sum_k x[r, k] * w[n, k] + bias[n]
+ *   out[r, n]   = act(y) + residual[r, n]
+ * Products run on the matrix core and are accumulated in fp32 (fp32 inputs in
+ * fp32 throughout); the epilogue is fp32 and out is rounded to nearest-even once.
+ * GRACE_E4M3 inputs with an output in bf16 take the 8-bit matrix instructions,
+ * which cut products far below the largest of their eight: a sum may be off by
+ * 2^-10 of sum |x w| (in the mean 1.4e-5 of the result); with an output in fp32
+ * the sums are those of fp32.
+ *
+ *   x          device, [R, K], dtype
+ *   x_scale    device, fp32 [R], or NULL (1): what a row's values are multiples
+ *              of, as grace_rms_norm writes it
+ *   w          device, [N, K], dtype
+ *   w_scale    device, fp32 [N], or NULL (1)
+ *   bias       device, [N], out_dtype, or NULL
+ *   residual   device, [R, N], out_dtype, or NULL; may be out itself (the stream
+ *              updated in place)
+ *   R, N, K    R >= 0 (0 is a no-op); N and K in 1 .. 2^30; R*N, R*K and
+ *              N*K below 2^40
+ *   act        enum grace_act
+ *   dtype      GRACE_F32, GRACE_BF16 or GRACE_E4M3 (x and w)
+ *   out_dtype  GRACE_F32 or GRACE_BF16
+ *   out        device, [R, N], out_dtype; must not overlap what is read, apart
+ *              from residual in place
+ *   stream     hipStream_t
+ */
+int32_t grace_linear(const void* x, const float* x_scale, const void* w, const float* w_scale,
+                     const void* bias, const void* residual, int32_t R, int32_t N, int32_t K,
+                     int32_t act, int32_t dtype, int32_t out_dtype, void* out, void* stream);
 
 /*
  * Graph capture (Sec. 5: the fixed-length decoding loop is captured as one

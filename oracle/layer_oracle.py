@@ -52,7 +52,8 @@ def linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale=Non
     elif act == "gelu":
         y = 0.5 * y * (1.0 + np.vectorize(math.erf)(y / math.sqrt(2.0))) if y.size else y
     elif act == "silu":
-        y = y / (1.0 + np.exp(-y))
+        with np.errstate(over="ignore"):
+            y = y / (1.0 + np.exp(-y))
     elif act != "none":
         raise ValueError(act)
     return y if residual is None else y + np.asarray(residual, dtype=np.float64)

@@ -519,4 +519,30 @@ int32_t grace_rms_norm(const void* x, const void* residual, const void* weight, 
                                            out, out_scale, (hipStream_t)stream));
 }
 
+int32_t grace_linear(const void* x, const float* x_scale, const void* w, const float* w_scale,
+                     const void* bias, const void* residual, int32_t R, int32_t N, int32_t K,
+                     int32_t act, int32_t dtype, int32_t out_dtype, void* out, void* stream) {
+  if (!good_dtype(dtype) || (out_dtype != GRACE_F32 && out_dtype != GRACE_BF16))
+    return GRACE_ERR_UNSUPPORTED;
+  if (act < GRACE_ACT_NONE || act > GRACE_ACT_SILU) return GRACE_ERR_UNSUPPORTED;
+  if (R < 0 || N < 1 || K < 1 || N > (1 << 30) || K > (1 << 30)) return GRACE_ERR_SHAPE;
+  constexpr int64_t kMost = (int64_t)1 << 40;
+  if ((int64_t)R * N >= kMost || (int64_t)R * K >= kMost || (int64_t)N * K >= kMost)
+    return GRACE_ERR_SHAPE;
+  if (R == 0) return GRACE_OK;
+  if (!x || !w || !out) return GRACE_ERR_NULL;
+  const int64_t in = elem_bytes(dtype), to = elem_bytes(out_dtype), n = (int64_t)R * N * to;
+  const Range reads[5] = {{x, (int64_t)R * K * in},
+                          {w, (int64_t)N * K * in},
+                          {x_scale, x_scale ? (int64_t)R * 4 : 0},
+                          {w_scale, w_scale ? (int64_t)N * 4 : 0},
+                          {bias, bias ? N * to : 0}};
+  for (const Range& r : reads)
+    if (overlaps(out, n, r.p, r.n)) return GRACE_ERR_ALIAS;
+  // the residual stream may be updated in place
+  if (residual && residual != out && overlaps(out, n, residual, n)) return GRACE_ERR_ALIAS;
+  return hip_status(grace::launch_linear(x, x_scale, w, w_scale, bias, residual, R, N, K, act,
+                                         dtype, out_dtype, out, (hipStream_t)stream));
+}
+
 }  // extern "C"

@@ -75,6 +75,14 @@ hipError_t launch_rms_norm(const void* x, const void* residual, const void* weig
                            void* out, float* out_scale, hipStream_t stream);
 int32_t rms_norm_max_d();
 
+// out [R, N] = act(x_scale w_scale x w^T + bias) + residual, x [R, K] and w [N, K]
+// in dtype, bias, residual and out in out_dtype; scales, bias and residual may be
+// null; residual may be out itself.
+hipError_t launch_linear(const void* x, const float* x_scale, const void* w, const float* w_scale,
+                         const void* bias, const void* residual, int32_t R, int32_t N, int32_t K,
+                         int32_t act, int32_t dtype, int32_t out_dtype, void* out,
+                         hipStream_t stream);
+
 // Debug builds: add the device-check counters of the attention kernels' source
 // files to acc[0 .. 7] and clear them (synchronous); release builds return
 // hipErrorNotSupported.

@@ -79,6 +79,8 @@ _SIGNATURES = {
     "grace_rms_norm_max_d": [],
     "grace_rms_norm": [_c_void_p, _c_void_p, _c_void_p, _c_int, _c_int, _c_float, _c_int, _c_int,
                        _c_void_p, _c_void_p, _c_void_p, _c_void_p],
+    "grace_linear": [_c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_int, _c_int,
+                     _c_int, _c_int, _c_int, _c_int, _c_void_p, _c_void_p],
     "grace_graph_begin": [_c_void_p],
     "grace_graph_end": [_c_void_p, ctypes.POINTER(_c_void_p)],
     "grace_graph_launch": [_c_void_p, _c_void_p],
@@ -493,6 +495,43 @@ def grace_rms_norm(x, weight, eps: float = 1e-6, residual=None, sum_out=None, ou
     _call("grace_rms_norm", x, _ptr(x), _ptr(residual), _ptr(weight), R, D, eps, code, out_code,
           _ptr(sum_out), _ptr(out), _ptr(out_scale))
     return (out, out_scale) if out_code == GRACE_E4M3 else out
+
+
+#: Activations of grace_linear (enum grace_act).
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+
+
+def grace_linear(x, w, bias=None, act: str = "none", residual=None, x_scale=None, w_scale=None,
+                 out=None, out_dtype=None):
+    """act(x_scale w_scale (x w^T) + bias) + residual; x [R, K] and w [N, K] of one
+    dtype (fp32, bf16 or float8_e4m3fn), x_scale fp32 [R], w_scale fp32 [N].
+    ``out_dtype`` (also bias's and residual's): out's dtype if given, else x's, or
+    bf16 for 8-bit inputs.  ``act``: a name in ACTIVATIONS.  ``residual`` may be out
+    itself.  Returns out [R, N]."""
+    (R, K), N = x.shape, w.shape[0]
+    dev, dtype = x.device, x.dtype
+    code = _ANY_DTYPE_CODE.get(dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    if out_dtype is None:
+        out_dtype = out.dtype if out is not None else torch.bfloat16 if code == GRACE_E4M3 else dtype
+    out_code = _DTYPE_CODE.get(out_dtype)
+    if out_code is None:
+        raise TypeError(f"unsupported dtype {out_dtype}")
+    if act not in ACTIVATIONS:
+        raise ValueError(f"unknown activation {act!r}")
+    if out is None:
+        out = torch.empty((R, N), dtype=out_dtype, device=dev)
+    _expect("x", x, (R, K), dtype, dev)
+    _expect("w", w, (N, K), dtype, dev)
+    _expect("bias", bias, (N,), out_dtype, dev)
+    _expect("residual", residual, (R, N), out_dtype, dev)
+    _expect("x_scale", x_scale, (R,), torch.float32, dev)
+    _expect("w_scale", w_scale, (N,), torch.float32, dev)
+    _expect("out", out, (R, N), out_dtype, dev)
+    _call("grace_linear", x, _ptr(x), _ptr(x_scale), _ptr(w), _ptr(w_scale), _ptr(bias),
+          _ptr(residual), R, N, K, ACTIVATIONS[act], code, out_code, _ptr(out))
+    return out
 
 
 class Graph:

@@ -93,3 +93,61 @@ def test_oracle_norm_closed_forms():
     assert (h == -2).all() and np.allclose(y, -1, rtol=1e-15)
     _, y = LO.rms_norm(np.array([[3.0, 4.0]]), np.array([2.0, 1.0]), 0.5)
     assert np.allclose(y, np.array([[6.0, 4.0]]) / math.sqrt(13.0), rtol=1e-15)
+
+
+def linear(**kw):
+    a = dict(x=at(1), xs=at(2), w=at(3), ws=at(4), bias=at(5), res=at(6), R=8, N=16, K=32, act=0,
+             dtype=G.GRACE_BF16, to=G.GRACE_BF16, out=at(7))
+    a.update(kw)
+    return G.library().grace_linear(a["x"], a["xs"], a["w"], a["ws"], a["bias"], a["res"], a["R"], a["N"],
+                                    a["K"], a["act"], a["dtype"], a["to"], a["out"], None)
+
+
+@needs_lib
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=3), G.GRACE_ERR_UNSUPPORTED), (dict(dtype=-1), G.GRACE_ERR_UNSUPPORTED),
+    (dict(to=2), G.GRACE_ERR_UNSUPPORTED), (dict(act=4), G.GRACE_ERR_UNSUPPORTED),
+    (dict(act=-1), G.GRACE_ERR_UNSUPPORTED), (dict(R=-1), G.GRACE_ERR_SHAPE),
+    (dict(N=0), G.GRACE_ERR_SHAPE), (dict(K=0), G.GRACE_ERR_SHAPE),
+    (dict(N=(1 << 30) + 1), G.GRACE_ERR_SHAPE), (dict(K=(1 << 30) + 1), G.GRACE_ERR_SHAPE),
+    (dict(R=1 << 30, N=1 << 10), G.GRACE_ERR_SHAPE), (dict(R=1 << 30, K=1 << 10), G.GRACE_ERR_SHAPE),
+    (dict(N=1 << 25, K=1 << 15), G.GRACE_ERR_SHAPE),
+    (dict(x=None), G.GRACE_ERR_NULL), (dict(w=None), G.GRACE_ERR_NULL), (dict(out=None), G.GRACE_ERR_NULL),
+    (dict(out=at(1)), G.GRACE_ERR_ALIAS), (dict(out=at(2)), G.GRACE_ERR_ALIAS),
+    (dict(out=at(3)), G.GRACE_ERR_ALIAS), (dict(out=at(4)), G.GRACE_ERR_ALIAS),
+    (dict(out=at(5)), G.GRACE_ERR_ALIAS),
+    (dict(out=ctypes.c_void_p((6 << 24) + 4)), G.GRACE_ERR_ALIAS),      # inside residual, not residual itself
+    (dict(R=0, x=None, out=None), G.GRACE_OK),
+])
+def test_linear_rejects(kw, status):
+    assert linear(**kw) == status
+
+
+def test_linear_binding_checks_every_tensor(monkeypatch):
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: calls.append(name) or 0
+
+    monkeypatch.setattr(G, "library", Library)
+    x, w = torch.zeros(4, 64), torch.zeros(8, 64)
+    for kw in (dict(w=torch.zeros(8, 63)), dict(bias=torch.zeros(4)), dict(residual=torch.zeros(8, 4)),
+               dict(x_scale=torch.zeros(8)), dict(w_scale=torch.zeros(4)), dict(out=torch.zeros(4, 9)),
+               dict(w=torch.zeros(64, 8).t()), dict(act="tanh")):
+        with pytest.raises(ValueError):
+            G.grace_linear(**{**dict(x=x, w=w), **kw})
+    for kw in (dict(w=w.bfloat16()), dict(bias=torch.zeros(8).bfloat16()), dict(x=x.half()),
+               dict(residual=torch.zeros(4, 8).double()), dict(x_scale=torch.zeros(4).bfloat16()),
+               dict(out_dtype=torch.float8_e4m3fn)):
+        with pytest.raises(TypeError):
+            G.grace_linear(**{**dict(x=x, w=w), **kw})
+    assert calls == []
+
+
+def test_oracle_linear_by_hand():
+    y = LO.linear([[1.0, 2.0]], [[3.0, -4.0]], bias=[1.0], act="relu", residual=[[0.5]])
+    assert y == 0.5                                       # 3 - 8 + 1 < 0
+    assert LO.linear([[1.0]], [[2.0]], x_scale=[3.0], w_scale=[5.0]) == 30.0
+    assert abs(LO.linear([[1.0]], [[1.0]], act="gelu") - 0.8413447460685429) < 1e-15
+    assert abs(LO.linear([[1.0]], [[1.0]], act="silu") - 0.7310585786300049) < 1e-15
