@@ -23,6 +23,8 @@
  *   grace_gtm_mask        decode-time constraint filter: constrained decoding on
  *                         the SID trie and target matching (Sec. 4, Sec. 5.4, App. A);
  *   grace_trie_advance    the trie node each selected beam moves to (Sec. 4.4);
+ *   grace_sample          a token per beam row, sampled from the filtered logits
+ *                         instead of searched for;
  *   grace_rms_norm        norm of the residual stream, with the residual's addition
  *                         and, if wanted, an output in 8 bits;
  *   grace_linear          matrix product (projections, feed-forward, logits) with
@@ -435,6 +437,62 @@ int32_t grace_trie_advance(const grace_gtm_index* index, const int32_t* node_pre
                            const int32_t* parents, const int32_t* tokens, int32_t B,
                            int32_t M_prev, int32_t k, int32_t* node_next, int32_t* err_flag,
                            void* stream);
+
+/* Bytes of device workspace grace_sample needs for B, M, V (-1 if out of range;
+ * may be 0). */
+int64_t grace_sample_workspace_bytes(int32_t B, int32_t M, int32_t V);
+
+/*
+ * Sampled continuation of every beam row, where grace_beam_step searches: row r =
+ * b*M + m draws one token from its logits under request b's rules.  (The rows then
+ * keep their places: the paged append takes parents m, the trie step takes
+ * M_prev = k = M.)
+ *
+ *   Candidates   tokens that the mask allows with a logit above -inf (a NaN is no
+ *                candidate), ordered by logit (descending), then token (ascending).
+ *   Weights      w_v = exp((z_v - z_best) / T); candidates of equal logits weigh
+ *                the same, also where they are +inf.
+ *   Kept         top_k: the first k of the order; then top_p: the shortest prefix
+ *                of these whose weights sum to at least p times theirs (the best
+ *                candidate always); then min_p: those with w >= min_p.
+ *   tokens[r]    the first kept token, in vocabulary order, whose running sum of
+ *                kept weights exceeds uniform[r] times their total.
+ *   scores[r]    prev_scores[r] + log_softmax(logits[r, :])[tokens[r]], over the
+ *                whole vocabulary at temperature 1, as grace_beam_scores; NaN where
+ *                the row has a NaN or +inf logit.
+ * A row without candidates gets token -1 and score -inf; grace_trie_advance takes
+ * it to node -1, a dead beam.  Every choice is the one that fp64 arithmetic makes.
+ *
+ *   logits       device, [B*M, V], dtype
+ *   uniform      device, fp32 [B*M]; random numbers in [0, 1) (others are clamped
+ *                into it, a NaN is 0)
+ *   prev_scores  device, fp32 [B*M], or NULL (0)
+ *   mask         device, uint32 [B*M, ceil(V/32)], or NULL: as for grace_beam_scores
+ *   temperature  device, fp32 [B], or NULL (1).  0, a negative value or a NaN takes
+ *                the best candidate
+ *   top_k        device, int32 [B], or NULL; values below 1 set no limit
+ *   top_p        device, fp32 [B], or NULL; values from 1 on set no limit, 0, negative
+ *                values and NaN keep the best candidate
+ *   min_p        device, fp32 [B], or NULL; 0, negative values and NaN set no limit,
+ *                values above 1 count as 1
+ *   B, M, V      requests, rows per request, vocabulary; B, M >= 0 (B*M = 0 is a
+ *                no-op), 1 <= V <= 2^24, B*M below 2^31, B*M*V below 2^40
+ *   dtype        GRACE_F32 or GRACE_BF16 (of the logits)
+ *   workspace    device, at least grace_sample_workspace_bytes(B, M, V) bytes,
+ *                8-byte aligned, caller-owned; contents on entry are ignored and on
+ *                return unspecified; calls that share it must not overlap (NULL
+ *                where none is needed)
+ *   tokens       device, int32 [B*M]
+ *   scores       device, fp32 [B*M]; may be prev_scores itself
+ *   stream       hipStream_t
+ * Apart from scores in place, outputs and the workspace must not overlap each
+ * other or the inputs.
+ */
+int32_t grace_sample(const void* logits, const float* uniform, const float* prev_scores,
+                     const uint32_t* mask, const float* temperature, const int32_t* top_k,
+                     const float* top_p, const float* min_p, int32_t B, int32_t M, int32_t V,
+                     int32_t dtype, void* workspace, int64_t workspace_bytes, int32_t* tokens,
+                     float* scores, void* stream);
 
 /* Longest row grace_rms_norm accepts (32768). */
 int32_t grace_rms_norm_max_d(void);

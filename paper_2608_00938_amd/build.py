@@ -16,7 +16,7 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libgrace.so")
 SOURCES = ["grace_api.hip", "cross_attn.hip", "self_attn.hip", "beam.hip", "graph.hip", "gtm.hip",
-           "norm.hip", "linear.hip"]
+           "norm.hip", "linear.hip", "sample.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -9,6 +9,7 @@ import pytest
 import torch
 
 from oracle import layer_oracle as LO
+from oracle import sample_oracle as SO
 from paper_2608_00938_amd import grace as G
 
 needs_lib = pytest.mark.skipif(not os.path.exists(G._LIB_PATH), reason="libgrace.so not built")
@@ -151,3 +152,93 @@ def test_oracle_linear_by_hand():
     assert LO.linear([[1.0]], [[2.0]], x_scale=[3.0], w_scale=[5.0]) == 30.0
     assert abs(LO.linear([[1.0]], [[1.0]], act="gelu") - 0.8413447460685429) < 1e-15
     assert abs(LO.linear([[1.0]], [[1.0]], act="silu") - 0.7310585786300049) < 1e-15
+
+
+def sample(**kw):
+    a = dict(z=at(1), u=at(2), prev=at(3), mask=at(4), T=at(5), k=at(6), p=at(7), m=at(8), B=2, M=4, V=64,
+             dtype=G.GRACE_BF16, ws=at(9), size=1 << 20, tok=at(10), sc=at(11))
+    a.update(kw)
+    return G.library().grace_sample(a["z"], a["u"], a["prev"], a["mask"], a["T"], a["k"], a["p"], a["m"],
+                                    a["B"], a["M"], a["V"], a["dtype"], a["ws"], a["size"], a["tok"], a["sc"],
+                                    None)
+
+
+@needs_lib
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=2), G.GRACE_ERR_UNSUPPORTED), (dict(B=-1), G.GRACE_ERR_SHAPE), (dict(M=-1), G.GRACE_ERR_SHAPE),
+    (dict(V=0), G.GRACE_ERR_SHAPE), (dict(V=(1 << 24) + 1), G.GRACE_ERR_SHAPE),
+    (dict(B=1 << 16, M=1 << 15), G.GRACE_ERR_SHAPE), (dict(B=1 << 10, M=1 << 10, V=1 << 20), G.GRACE_ERR_SHAPE),
+    (dict(z=None), G.GRACE_ERR_NULL), (dict(u=None), G.GRACE_ERR_NULL), (dict(tok=None), G.GRACE_ERR_NULL),
+    (dict(sc=None), G.GRACE_ERR_NULL),
+    (dict(tok=at(1)), G.GRACE_ERR_ALIAS), (dict(tok=at(2)), G.GRACE_ERR_ALIAS),
+    (dict(tok=at(3)), G.GRACE_ERR_ALIAS), (dict(sc=at(4)), G.GRACE_ERR_ALIAS),
+    (dict(sc=at(5)), G.GRACE_ERR_ALIAS), (dict(sc=at(6)), G.GRACE_ERR_ALIAS),
+    (dict(sc=at(7)), G.GRACE_ERR_ALIAS), (dict(tok=at(8)), G.GRACE_ERR_ALIAS),
+    (dict(sc=at(10)), G.GRACE_ERR_ALIAS),
+    (dict(sc=ctypes.c_void_p((3 << 24) + 4)), G.GRACE_ERR_ALIAS),       # inside prev, not prev itself
+    (dict(B=0, z=None), G.GRACE_OK), (dict(M=0, tok=None), G.GRACE_OK),
+])
+def test_sample_rejects(kw, status):
+    assert sample(**kw) == status
+
+
+@needs_lib
+def test_sample_workspace():
+    lib = G.library()
+    assert lib.grace_sample_workspace_bytes(-1, 1, 8) == -1
+    assert lib.grace_sample_workspace_bytes(1, 1, 0) == -1
+    assert lib.grace_sample_workspace_bytes(1 << 16, 1 << 15, 8) == -1
+    for B, M, V in ((0, 1, 8), (1, 1, 1 << 24), (64, 4096, 512), (1, 1, 128000)):
+        need = lib.grace_sample_workspace_bytes(B, M, V)
+        assert 0 <= need < 1 << 30
+        if need > 0:
+            kw = dict(B=B, M=M, V=V, u=at(64), prev=at(96), mask=at(128), T=at(192), k=at(193), p=at(194),
+                      m=at(195), tok=at(200), sc=at(216), ws=at(256))
+            assert sample(**kw, size=need - 1) == G.GRACE_ERR_SHAPE
+            assert sample(**{**kw, "ws": None}, size=need) == G.GRACE_ERR_NULL
+            assert sample(**{**kw, "ws": ctypes.c_void_p((256 << 24) + 4)}, size=need) == G.GRACE_ERR_SHAPE
+            assert sample(**{**kw, "ws": at(1)}, size=need) == G.GRACE_ERR_ALIAS
+
+
+def test_sample_binding_checks_every_tensor(monkeypatch):
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: calls.append(name) or 0
+
+    monkeypatch.setattr(G, "library", Library)
+    i32 = torch.int32
+    z, u = torch.zeros(6, 40), torch.zeros(6)
+    for kw in (dict(B=3), dict(uniform=torch.zeros(5)), dict(prev_scores=torch.zeros(2)),
+               dict(mask=torch.zeros(6, 1, dtype=i32)), dict(temperature=torch.zeros(6)),
+               dict(top_k=torch.zeros(6, dtype=i32)), dict(top_p=torch.zeros(3)), dict(min_p=torch.zeros(1)),
+               dict(tokens=torch.zeros(7, dtype=i32)), dict(scores=torch.zeros(2, 3)),
+               dict(logits=torch.zeros(40, 6).t())):
+        with pytest.raises(ValueError):
+            G.grace_sample(**{**dict(logits=z, uniform=u, B=2, M=3), **kw})
+    for kw in (dict(logits=z.half()), dict(uniform=u.double()), dict(top_k=torch.zeros(2)),
+               dict(mask=torch.zeros(6, 2, dtype=torch.int64)), dict(tokens=torch.zeros(6, dtype=torch.int64)),
+               dict(temperature=torch.zeros(2).bfloat16())):
+        with pytest.raises(TypeError):
+            G.grace_sample(**{**dict(logits=z, uniform=u, B=2, M=3), **kw})
+    assert calls == []
+
+
+def test_oracle_sampling_by_hand():
+    z = np.log(np.array([0.1, 0.4, 0.2, 0.3]))
+    pick = lambda u, **kw: SO.sample_row(z, u, **kw)  # noqa: E731
+    assert [pick(u) for u in (0.0, 0.09, 0.11, 0.49, 0.51, 0.69, 0.71, 0.999)] == [0, 0, 1, 1, 2, 2, 3, 3]
+    assert list(SO.kept_tokens(z, k=2)[0]) == [1, 3]
+    assert [pick(u, k=2) for u in (0.0, 0.57, 0.58)] == [1, 1, 3]          # 4/7
+    assert list(SO.kept_tokens(z, p=0.65)[0]) == [1, 3] and list(SO.kept_tokens(z, p=0.75)[0]) == [1, 3, 2]
+    assert list(SO.kept_tokens(z, k=3, p=0.75)[0]) == [1, 3]               # 0.7 of 0.9 reaches 0.675
+    assert list(SO.kept_tokens(z, min_p=0.45)[0]) == [1, 3, 2]
+    assert list(SO.kept_tokens(z, T=0.0)[0]) == [1] and list(SO.kept_tokens(z, p=0.0)[0]) == [1]
+    assert list(SO.kept_tokens(z, allowed=[1, 0, 1, 0])[0]) == [2, 0]
+    assert pick(0.5, allowed=[0, 0, 0, 0]) == -1
+    w = SO.kept_tokens(z, T=0.5)[1]                                        # squares of the odds
+    assert np.allclose(w, np.array([1, 9 / 16, 1 / 4, 1 / 16]))
+    # ties: the lower token first, and equal logits weigh the same
+    assert list(SO.kept_tokens(np.zeros(4), k=3)[0]) == [0, 1, 2]
+    assert list(SO.kept_tokens(np.zeros(4), p=0.5)[0]) == [0, 1]
