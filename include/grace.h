@@ -469,7 +469,7 @@ int64_t grace_sample_workspace_bytes(int32_t B, int32_t M, int32_t V);
  *   prev_scores  device, fp32 [B*M], or NULL (0)
  *   mask         device, uint32 [B*M, ceil(V/32)], or NULL: as for grace_beam_scores
  *   temperature  device, fp32 [B], or NULL (1).  0, a negative value or a NaN takes
- *                the best candidate
+ *                the best candidate; +inf counts as the largest fp32
  *   top_k        device, int32 [B], or NULL; values below 1 set no limit
  *   top_p        device, fp32 [B], or NULL; values from 1 on set no limit, 0, negative
  *                values and NaN keep the best candidate
