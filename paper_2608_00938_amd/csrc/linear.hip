@@ -105,6 +105,21 @@ __device__ __forceinline__ float activate(float y, int act) {
   return y;
 }
 
+// The same for four values, the choice made once.
+__device__ __forceinline__ void activate4(float* y, int act) {
+  if (act == GRACE_ACT_NONE) return;
+  if (act == GRACE_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = y[e] < 0.f ? 0.f : y[e];
+  } else if (act == GRACE_ACT_GELU) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = activate(y[e], GRACE_ACT_GELU);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = activate(y[e], GRACE_ACT_SILU);
+  }
+}
+
 __device__ __forceinline__ float load_out_type(const void* p, int64_t i, int dtype) {
   return dtype == GRACE_F32 ? ((const float*)p)[i] : bf16_bits_to_f32(((const uint16_t*)p)[i]);
 }
@@ -222,11 +237,268 @@ __global__ void __launch_bounds__(256) linear_kernel(LinearArgs a) {
   }
 }
 
-template <class T>
+// ---------------------------------------------------------------------------
+// Tile kernel: direct loads into a ring of LDS tiles.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+// 16 bytes per lane from base + off to LDS at `to` + 16 * lane (base and `to`
+// uniform over the wave).  As asm, so that the compiler does not wait for it where
+// LDS is read: wait_loads does, ahead of the barrier that hands the tile on.
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, uint32_t to) {
+  asm volatile("global_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "{m0}"(to) : "memory");
+}
+// Waits until at most N of the wave's loads are under way.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// Which tile a workgroup takes.  Workgroup i runs on XCD i % 8: each XCD takes a
+// contiguous eighth of the tiles, and these go through groups of 8 row tiles, one
+// column of the group after the other, so that the 64 workgroups an XCD runs at once
+// read 8 row tiles and 8 column tiles through its L2.
+struct TileMap {
+  int64_t tiles_r, tiles_n;
+  __device__ bool take(int64_t id, int64_t& tr, int64_t& tn) const {
+    const int64_t all = tiles_r * tiles_n, per = (all + 7) / 8;
+    const int64_t i = id % 8 * per + id / 8;
+    if (id / 8 >= per || i >= all) return false;
+    const int64_t group = i / (8 * tiles_n), in = i % (8 * tiles_n);
+    const int64_t high = min((int64_t)8, tiles_r - group * 8);
+    tr = group * 8 + in % high;
+    tn = in / high;
+    return true;
+  }
+};
+
+// Four values from 4-aligned element i of a tensor of O's type.
+template <class O>
+__device__ __forceinline__ void load4(const void* p, int64_t i, float* f) {
+  if constexpr (O::kBytes == 4) {
+    const f32x4 v = *(const f32x4*)((const float*)p + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = v[e];
+  } else {
+    const u32x2 v = *(const u32x2*)((const uint16_t*)p + i);
+    f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
+    f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
+  }
+}
+
+// WR x WN waves of RT x NT tiles of 32 x 32: BR rows of x against BN rows of w, in
+// steps of 64 bytes of k that pass through a ring of three LDS tiles, two ahead of
+// the products.  Two workgroups share a CU, so that the matrix core has one's
+// products where the other waits, loads its first fragments or runs its epilogue.
+//
+// Needs 16-byte aligned rows of x and w (k a multiple of a chunk); VEC: outputs
+// whose rows are a multiple of 8 elements and, with bias and residual, 16-byte
+// aligned, which leave through LDS as whole lines.
+template <class T, class O, int WR, int WN, int RT, int NT, bool VEC>
+__global__ void __launch_bounds__(256, 2) linear_tile_kernel(LinearArgs a, TileMap map) {
+  static_assert(WR * WN == 4, "four waves");
+  using S = Step<T>;
+  constexpr int BR = WR * RT * 32, BN = WN * NT * 32, kRows = BR + BN;
+  constexpr int kChunks = 4, kLoads = kRows * kChunks / 256, kStages = 3;
+  constexpr int kStageBytes = kRows * 64, kSteps = S::kSteps / 2;
+  constexpr int kOutRow = NT * 32 * O::kBytes;             // a wave's output row in LDS
+  constexpr int kOutBytes = VEC ? 4 * 32 * kOutRow : 0;
+  constexpr int kLds = kStages * kStageBytes > kOutBytes ? kStages * kStageBytes : kOutBytes;
+  __shared__ __attribute__((aligned(256))) char lds[kLds];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = lane >> 5, col = lane & 31;
+  int64_t tr, tn;
+  if (!map.take(blockIdx.x, tr, tn)) return;
+  const int64_t r0 = tr * BR;
+  const int32_t n0 = (int32_t)(tn * BN);
+
+  // Loads: a wave's instruction covers 16 rows; lane l brings row l / 4's chunk to
+  // place l % 4, where chunk c of row r lies at place c ^ (r / 4 % 4): 16 rows of one
+  // chunk, as a fragment's lanes read them, are on different banks.
+  const int64_t pitch = (int64_t)a.K * T::kBytes;
+  const int chunk = (lane & 3) ^ (lane >> 4 & 3);
+  const char* const xb = (const char*)a.x + r0 * pitch;
+  const char* const wb = (const char*)a.w + (int64_t)n0 * pitch;
+  uint32_t off[kLoads];
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    const int row = (wave + j * 4) * 16 + (lane >> 2);
+    const int64_t in = (wave + j * 4) * 16 < BR ? min((int64_t)row, (int64_t)a.R - 1 - r0)
+                                                : min((int64_t)row - BR, (int64_t)a.N - 1 - n0);
+    off[j] = (uint32_t)(in * pitch) + chunk * 16;
+  }
+  const int32_t tiles = (int32_t)((pitch + 63) / 64);
+  const int last_chunks = (int)((pitch - (int64_t)(tiles - 1) * 64) / 16);
+  const bool beyond = chunk >= last_chunks;                // in the last tile: past k's end
+  const uint32_t lds0 = lds_addr(lds);
+  const auto issue = [&](int32_t t, int stage) {
+    const int64_t at = (int64_t)t * 64;
+    // what lies past a row's end reads the row's first chunk of the tile, and is cleared later
+    const uint32_t back = t == tiles - 1 && beyond ? chunk * 16 : 0;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      load_to_lds(((wave + j * 4) * 16 < BR ? xb : wb) + at, off[j] - back,
+                  lds0 + stage * kStageBytes + (wave + j * 4) * 1024);
+  };
+  const auto clear_beyond = [&](int stage) {
+    if (beyond)
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+        *(u32x4*)(lds + stage * kStageBytes + (wave + j * 4) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+  };
+
+  f32x16 acc[RT][NT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x16{0};
+  const int wr = wave / WN * RT * 32, wn = wave % WN * NT * 32;
+  const int swz = col >> 2 & 3;
+  issue(0, 0);
+  if (tiles > 1) issue(1, 1);
+  if (tiles > 1) wait_loads<kLoads>();
+  else wait_loads<0>();
+  if (tiles == 1) clear_beyond(0);
+  lds_barrier();
+  int stage = 0;
+  for (int32_t t = 0; t < tiles; ++t) {
+    const int ahead = stage == 0 ? 2 : stage - 1, next = stage == 2 ? 0 : stage + 1;
+    if (t + 2 < tiles) issue(t + 2, ahead);
+    const char* const xs = lds + stage * kStageBytes + (wr + col) * 64;
+    const char* const ws = lds + stage * kStageBytes + (BR + wn + col) * 64;
+    typename S::Frag fr[kSteps][RT], fn[kSteps][NT];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const auto frag = [&](const char* p) {
+        u32x4 c[S::kChunks];
+#pragma unroll
+        for (int i = 0; i < S::kChunks; ++i)
+          c[i] = *(const u32x4*)(p + (((s * 2 + half) * S::kChunks + i) ^ swz) * 16);
+        return S::make(c);
+      };
+#pragma unroll
+      for (int j = 0; j < NT; ++j) fn[s][j] = frag(ws + j * 32 * 64);
+#pragma unroll
+      for (int i = 0; i < RT; ++i) fr[s][i] = frag(xs + i * 32 * 64);
+    }
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = S::run(fn[s][j], fr[s][i], acc[i][j]);
+    if (t + 2 < tiles) wait_loads<kLoads>();
+    else wait_loads<0>();
+    if (t + 2 == tiles) clear_beyond(next);
+    lds_barrier();
+    stage = next;
+  }
+
+  // Epilogue in the accumulators' layout: lane l has rows r = l % 32 and, of every 8
+  // columns, 4 (l / 32) .. + 3.
+  if constexpr (VEC) {
+    char* const mine = lds + wave * 32 * kOutRow;
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      const int64_t r = min(r0 + wr + i * 32 + col, (int64_t)a.R - 1);
+      const float xs = a.x_scale ? a.x_scale[r] : 1.f;
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int32_t n = min(n0 + wn + j * 32 + g * 8 + half * 4, a.N - 4);
+          float y[4], v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = acc[i][j][g * 4 + e] * xs;
+          if (a.w_scale) {
+            load4<F32>(a.w_scale, n, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] *= v[e];
+          }
+          if (a.bias) {
+            load4<O>(a.bias, n, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] += v[e];
+          }
+          activate4(y, a.act);
+          if (a.residual) {
+            load4<O>(a.residual, r * a.N + n, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] += v[e];
+          }
+          // 16-byte chunks of a row, swizzled over the rows
+          constexpr int kRowChunk = kOutRow / 16;
+          const int byte = (j * 32 + g * 8 + half * 4) * O::kBytes;
+          char* const to = mine + col * kOutRow + ((byte / 16) ^ (col >> 1 & (kRowChunk - 1))) * 16 + byte % 16;
+          if constexpr (O::kBytes == 4) *(f32x4*)to = f32x4{y[0], y[1], y[2], y[3]};
+          else *(u32x2*)to = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+        }
+      // whole lines of the wave's 32 rows
+      constexpr int kRowChunk = kOutRow / 16, kPer = 32 * kRowChunk / 64;
+#pragma unroll
+      for (int q = 0; q < kPer; ++q) {
+        const int row = (q * 64 + lane) / kRowChunk, c = lane % kRowChunk;
+        const u32x4 v = *(const u32x4*)(mine + row * kOutRow + (c ^ (row >> 1 & (kRowChunk - 1))) * 16);
+        const int64_t r = r0 + wr + i * 32 + row;
+        const int32_t n = n0 + wn + c * (16 / O::kBytes);
+        if (r < a.R && n < a.N) *(u32x4*)((char*)a.out + (r * a.N + n) * O::kBytes) = v;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      const int64_t r = r0 + wr + i * 32 + col;
+      if (r >= a.R) continue;
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float v[4] = {acc[i][j][g * 4], acc[i][j][g * 4 + 1], acc[i][j][g * 4 + 2],
+                              acc[i][j][g * 4 + 3]};
+          finish4(a, r, n0 + wn + j * 32 + g * 8 + half * 4, v);
+        }
+    }
+  }
+}
+
+template <class T, class O, int WR, int WN, int RT, int NT>
+hipError_t run_tile(const LinearArgs& a, hipStream_t stream) {
+  constexpr int BR = WR * RT * 32, BN = WN * NT * 32;
+  const TileMap map{((int64_t)a.R + BR - 1) / BR, ((int64_t)a.N + BN - 1) / BN};
+  const uint32_t grid = (uint32_t)((map.tiles_r * map.tiles_n + 7) / 8 * 8);
+  const uintptr_t any = (uintptr_t)a.out | (uintptr_t)a.bias | (uintptr_t)a.residual | (uintptr_t)a.w_scale;
+  if (a.N % 8 == 0 && any % 16 == 0)
+    linear_tile_kernel<T, O, WR, WN, RT, NT, true><<<grid, 256, 0, stream>>>(a, map);
+  else
+    linear_tile_kernel<T, O, WR, WN, RT, NT, false><<<grid, 256, 0, stream>>>(a, map);
+  return hipGetLastError();
+}
+
+template <class T, class O>
 hipError_t run(const LinearArgs& a, hipStream_t stream) {
+  // rows that start on 16 bytes, and a tile of them within 32-bit offsets
+  const int64_t pitch = (int64_t)a.K * T::kBytes;
+  const bool direct = pitch % 16 == 0 && ((uintptr_t)a.x | (uintptr_t)a.w) % 16 == 0 && pitch < (1 << 22);
+  if (direct) {
+    const auto tiles = [&](int br, int bn) {
+      return ((int64_t)a.R + br - 1) / br * (((int64_t)a.N + bn - 1) / bn);
+    };
+    if (tiles(256, 128) >= 512) return run_tile<T, O, 2, 2, 4, 2>(a, stream);
+    if (tiles(128, 128) >= 256) return run_tile<T, O, 2, 2, 2, 2>(a, stream);
+    return run_tile<T, O, 2, 2, 1, 1>(a, stream);
+  }
   const int64_t tiles = (((int64_t)a.R + 63) / 64) * (((int64_t)a.N + 63) / 64);
   linear_kernel<T, 2, 2, 1, 1><<<(uint32_t)tiles, 256, 0, stream>>>(a);
   return hipGetLastError();
+}
+
+template <class T>
+hipError_t run_out(const LinearArgs& a, hipStream_t stream) {
+  return a.out_dtype == GRACE_F32 ? run<T, F32>(a, stream) : run<T, BF16>(a, stream);
 }
 
 }  // namespace
@@ -236,9 +508,9 @@ hipError_t launch_linear(const void* x, const float* x_scale, const void* w, con
                          int32_t act, int32_t dtype, int32_t out_dtype, void* out,
                          hipStream_t stream) {
   const LinearArgs a{x, w, x_scale, w_scale, bias, residual, out, R, N, K, act, out_dtype};
-  if (dtype == GRACE_F32) return run<F32>(a, stream);
-  if (dtype == GRACE_BF16) return run<BF16>(a, stream);
-  return out_dtype == GRACE_BF16 ? run<E4M3>(a, stream) : run<E4M3Wide>(a, stream);
+  if (dtype == GRACE_F32) return run_out<F32>(a, stream);
+  if (dtype == GRACE_BF16) return run_out<BF16>(a, stream);
+  return out_dtype == GRACE_BF16 ? run<E4M3, BF16>(a, stream) : run<E4M3Wide, F32>(a, stream);
 }
 
 }  // namespace grace
