@@ -222,6 +222,11 @@ __global__ void __launch_bounds__(256) linear_kernel(LinearArgs a) {
         for (int j = 0; j < NT; ++j) acc[i][j] = S::run(fn[j], fr[i], acc[i][j]);
     }
   }
+  // (see linear_tile_kernel)
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(acc[i][j]));
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
     const int64_t r = r0 + wr + i * 32 + col;
@@ -291,23 +296,31 @@ __device__ __forceinline__ void load4(const void* p, int64_t i, float* f) {
 }
 
 // WR x WN waves of RT x NT tiles of 32 x 32: BR rows of x against BN rows of w, in
-// steps of 64 bytes of k that pass through a ring of three LDS tiles, two ahead of
-// the products.  Two workgroups share a CU, so that the matrix core has one's
-// products where the other waits, loads its first fragments or runs its epilogue.
+// tiles of 128 bytes of k (whole cache lines: with 64 the L2 had twice the requests
+// to serve and was the bound) that alternate between two LDS stages.
+//
+// Order within a wave.  The products of a step go through the rows of the wave's
+// tile; when a row is done its fragment of the next step is read into the same
+// registers, the columns' fragments into a second set.  In a tile's last step the
+// first row's products are followed by the hand-over: the next tile has landed and
+// every wave has the rest of this one in registers (one barrier).  From there to the
+// end of the next tile's first step the loads of the tile after next are issued into
+// the stage just left, one or two after each row: all at once they fill the address
+// path's queue and hold up the waves behind them (8192^3 bf16 973 us).
 //
 // Needs 16-byte aligned rows of x and w (k a multiple of a chunk); VEC: outputs
 // whose rows are a multiple of 8 elements and, with bias and residual, 16-byte
 // aligned, which leave through LDS as whole lines.
 template <class T, class O, int WR, int WN, int RT, int NT, bool VEC>
-__global__ void __launch_bounds__(256, 2) linear_tile_kernel(LinearArgs a, TileMap map) {
-  static_assert(WR * WN == 4, "four waves");
+__global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs a, TileMap map) {
   using S = Step<T>;
+  constexpr int kTileWaves = WR * WN;
   constexpr int BR = WR * RT * 32, BN = WN * NT * 32, kRows = BR + BN;
-  constexpr int kChunks = 4, kLoads = kRows * kChunks / 256, kStages = 3;
-  constexpr int kStageBytes = kRows * 64, kSteps = S::kSteps / 2;
+  constexpr int kLoads = kRows / (kTileWaves * 8);         // of 8 rows
+  constexpr int kStageBytes = kRows * 128;
   constexpr int kOutRow = NT * 32 * O::kBytes;             // a wave's output row in LDS
-  constexpr int kOutBytes = VEC ? 4 * 32 * kOutRow : 0;
-  constexpr int kLds = kStages * kStageBytes > kOutBytes ? kStages * kStageBytes : kOutBytes;
+  constexpr int kOutBytes = VEC ? kTileWaves * 32 * kOutRow : 0;
+  constexpr int kLds = 2 * kStageBytes > kOutBytes ? 2 * kStageBytes : kOutBytes;
   __shared__ __attribute__((aligned(256))) char lds[kLds];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, col = lane & 31;
@@ -316,39 +329,45 @@ __global__ void __launch_bounds__(256, 2) linear_tile_kernel(LinearArgs a, TileM
   const int64_t r0 = tr * BR;
   const int32_t n0 = (int32_t)(tn * BN);
 
-  // Loads: a wave's instruction covers 16 rows; lane l brings row l / 4's chunk to
-  // place l % 4, where chunk c of row r lies at place c ^ (r / 4 % 4): 16 rows of one
+  // Loads: a wave's instruction covers 8 rows; lane l brings a chunk of row l / 8 to
+  // place l % 8, where chunk c of row r lies at place c ^ (r / 2 % 8): 16 rows of one
   // chunk, as a fragment's lanes read them, are on different banks.
   const int64_t pitch = (int64_t)a.K * T::kBytes;
-  const int chunk = (lane & 3) ^ (lane >> 4 & 3);
+  const int chunk = (lane & 7) ^ ((wave * 4 + (lane >> 4)) & 7);
   const char* const xb = (const char*)a.x + r0 * pitch;
   const char* const wb = (const char*)a.w + (int64_t)n0 * pitch;
   uint32_t off[kLoads];
 #pragma unroll
   for (int j = 0; j < kLoads; ++j) {
-    const int row = (wave + j * 4) * 16 + (lane >> 2);
-    const int64_t in = (wave + j * 4) * 16 < BR ? min((int64_t)row, (int64_t)a.R - 1 - r0)
-                                                : min((int64_t)row - BR, (int64_t)a.N - 1 - n0);
+    const int row = (wave + j * kTileWaves) * 8 + (lane >> 3);
+    const int64_t in = (wave + j * kTileWaves) * 8 < BR ? min((int64_t)row, (int64_t)a.R - 1 - r0)
+                                                        : min((int64_t)row - BR, (int64_t)a.N - 1 - n0);
     off[j] = (uint32_t)(in * pitch) + chunk * 16;
   }
-  const int32_t tiles = (int32_t)((pitch + 63) / 64);
-  const int last_chunks = (int)((pitch - (int64_t)(tiles - 1) * 64) / 16);
+  const int32_t tiles = (int32_t)((pitch + 127) / 128);
+  const int last_chunks = (int)((pitch - (int64_t)(tiles - 1) * 128) / 16);
   const bool beyond = chunk >= last_chunks;                // in the last tile: past k's end
   const uint32_t lds0 = lds_addr(lds);
-  const auto issue = [&](int32_t t, int stage) {
-    const int64_t at = (int64_t)t * 64;
+  const auto load = [&](int32_t t, int j) {
     // what lies past a row's end reads the row's first chunk of the tile, and is cleared later
     const uint32_t back = t == tiles - 1 && beyond ? chunk * 16 : 0;
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j)
-      load_to_lds(((wave + j * 4) * 16 < BR ? xb : wb) + at, off[j] - back,
-                  lds0 + stage * kStageBytes + (wave + j * 4) * 1024);
+    load_to_lds(((wave + j * kTileWaves) * 8 < BR ? xb : wb) + (int64_t)t * 128, off[j] - back,
+                lds0 + (t & 1) * kStageBytes + (wave + j * kTileWaves) * 1024);
   };
-  const auto clear_beyond = [&](int stage) {
-    if (beyond)
+  constexpr int kPerRow = (kLoads + 2 * RT - 1) / (2 * RT); // loads after a row's products
+  const auto load_part = [&](int32_t t, int part) {
+#pragma unroll
+    for (int j = part * kPerRow; j < (part + 1) * kPerRow; ++j)
+      if (j < kLoads) load(t, j);
+  };
+  // Tile t has landed, its end of k is clean, and every wave knows it.
+  const auto hand_over = [&](int32_t t) {
+    wait_loads<0>();
+    if (t == tiles - 1 && beyond)
 #pragma unroll
       for (int j = 0; j < kLoads; ++j)
-        *(u32x4*)(lds + stage * kStageBytes + (wave + j * 4) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+        *(u32x4*)(lds + (t & 1) * kStageBytes + (wave + j * kTileWaves) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+    lds_barrier();
   };
 
   f32x16 acc[RT][NT];
@@ -357,46 +376,66 @@ __global__ void __launch_bounds__(256, 2) linear_tile_kernel(LinearArgs a, TileM
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x16{0};
   const int wr = wave / WN * RT * 32, wn = wave % WN * NT * 32;
-  const int swz = col >> 2 & 3;
-  issue(0, 0);
-  if (tiles > 1) issue(1, 1);
-  if (tiles > 1) wait_loads<kLoads>();
-  else wait_loads<0>();
-  if (tiles == 1) clear_beyond(0);
-  lds_barrier();
-  int stage = 0;
-  for (int32_t t = 0; t < tiles; ++t) {
-    const int ahead = stage == 0 ? 2 : stage - 1, next = stage == 2 ? 0 : stage + 1;
-    if (t + 2 < tiles) issue(t + 2, ahead);
-    const char* const xs = lds + stage * kStageBytes + (wr + col) * 64;
-    const char* const ws = lds + stage * kStageBytes + (BR + wn + col) * 64;
-    typename S::Frag fr[kSteps][RT], fn[kSteps][NT];
+  const int swz = col >> 1 & 7;
+  const char* const xrow = lds + (wr + col) * 128;
+  const char* const wrow = lds + (BR + wn + col) * 128;
+  typename S::Frag fr[RT], fn[2][NT];
+  const auto frag = [&](const char* row, int stage, int s) {
+    u32x4 c[S::kChunks];
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const auto frag = [&](const char* p) {
-        u32x4 c[S::kChunks];
+    for (int i = 0; i < S::kChunks; ++i)
+      c[i] = *(const u32x4*)(row + stage * kStageBytes + (((s * 2 + half) * S::kChunks + i) ^ swz) * 16);
+    return S::make(c);
+  };
+  // tile t; next: there is a tile behind it, more: and one behind that
+  const auto tile = [&](int32_t t, auto next, auto more) {
+    const int stage = t & 1;
 #pragma unroll
-        for (int i = 0; i < S::kChunks; ++i)
-          c[i] = *(const u32x4*)(p + (((s * 2 + half) * S::kChunks + i) ^ swz) * 16);
-        return S::make(c);
-      };
+    for (int s = 0; s < S::kSteps; ++s) {
+      const bool last = s + 1 == S::kSteps;
+      const int from = last ? stage ^ 1 : stage, step = last ? 0 : s + 1;
 #pragma unroll
-      for (int j = 0; j < NT; ++j) fn[s][j] = frag(ws + j * 32 * 64);
+      for (int i = 0; i < RT; ++i) {
 #pragma unroll
-      for (int i = 0; i < RT; ++i) fr[s][i] = frag(xs + i * 32 * 64);
+        for (int j = 0; j < NT; ++j) acc[i][j] = S::run(fn[s & 1][j], fr[i], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (!last || next) {
+          if (i == 0) {
+            if (last) hand_over(t + 1);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) fn[(s + 1) & 1][j] = frag(wrow + j * 32 * 128, from, step);
+          }
+          fr[i] = frag(xrow + i * 32 * 128, from, step);
+        }
+        if (last && more) load_part(t + 2, i);
+        if (s == 0 && next) load_part(t + 1, RT + i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
+  };
+  struct Yes { constexpr operator bool() const { return true; } };
+  struct No { constexpr operator bool() const { return false; } };
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s)
+  for (int j = 0; j < kLoads; ++j) load(0, j);
+  hand_over(0);
+  if (tiles > 1)
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+    for (int i = 0; i < RT; ++i) load_part(1, i);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = S::run(fn[s][j], fr[s][i], acc[i][j]);
-    if (t + 2 < tiles) wait_loads<kLoads>();
-    else wait_loads<0>();
-    if (t + 2 == tiles) clear_beyond(next);
-    lds_barrier();
-    stage = next;
-  }
+  for (int j = 0; j < NT; ++j) fn[0][j] = frag(wrow + j * 32 * 128, 0, 0);
+#pragma unroll
+  for (int i = 0; i < RT; ++i) fr[i] = frag(xrow + i * 32 * 128, 0, 0);
+  int32_t t = 0;
+  for (; t + 2 < tiles; ++t) tile(t, Yes{}, Yes{});
+  if (t + 1 < tiles) tile(t++, Yes{}, No{});
+  tile(t, No{}, No{});
+  // The products stay out of the epilogue's branches: there the compiler would set the
+  // block scales for the lanes that store alone, and the matrix core reads all lanes'.
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(acc[i][j]));
+  lds_barrier();
 
   // Epilogue in the accumulators' layout: lane l has rows r = l % 32 and, of every 8
   // columns, 4 (l / 32) .. + 3.
@@ -467,14 +506,14 @@ __global__ void __launch_bounds__(256, 2) linear_tile_kernel(LinearArgs a, TileM
 
 template <class T, class O, int WR, int WN, int RT, int NT>
 hipError_t run_tile(const LinearArgs& a, hipStream_t stream) {
-  constexpr int BR = WR * RT * 32, BN = WN * NT * 32;
+  constexpr int BR = WR * RT * 32, BN = WN * NT * 32, kThreads = WR * WN * 64;
   const TileMap map{((int64_t)a.R + BR - 1) / BR, ((int64_t)a.N + BN - 1) / BN};
   const uint32_t grid = (uint32_t)((map.tiles_r * map.tiles_n + 7) / 8 * 8);
   const uintptr_t any = (uintptr_t)a.out | (uintptr_t)a.bias | (uintptr_t)a.residual | (uintptr_t)a.w_scale;
   if (a.N % 8 == 0 && any % 16 == 0)
-    linear_tile_kernel<T, O, WR, WN, RT, NT, true><<<grid, 256, 0, stream>>>(a, map);
+    linear_tile_kernel<T, O, WR, WN, RT, NT, true><<<grid, kThreads, 0, stream>>>(a, map);
   else
-    linear_tile_kernel<T, O, WR, WN, RT, NT, false><<<grid, 256, 0, stream>>>(a, map);
+    linear_tile_kernel<T, O, WR, WN, RT, NT, false><<<grid, kThreads, 0, stream>>>(a, map);
   return hipGetLastError();
 }
 
@@ -487,7 +526,7 @@ hipError_t run(const LinearArgs& a, hipStream_t stream) {
     const auto tiles = [&](int br, int bn) {
       return ((int64_t)a.R + br - 1) / br * (((int64_t)a.N + bn - 1) / bn);
     };
-    if (tiles(256, 128) >= 512) return run_tile<T, O, 2, 2, 4, 2>(a, stream);
+    if (tiles(256, 256) >= 256) return run_tile<T, O, 2, 4, 4, 2>(a, stream);
     if (tiles(128, 128) >= 256) return run_tile<T, O, 2, 2, 2, 2>(a, stream);
     return run_tile<T, O, 2, 2, 1, 1>(a, stream);
   }
