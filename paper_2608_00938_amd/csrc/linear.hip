@@ -105,18 +105,38 @@ __device__ __forceinline__ float activate(float y, int act) {
   return y;
 }
 
-// The same for four values, the choice made once.
-__device__ __forceinline__ void activate4(float* y, int act) {
+// N values, the choice made once.  Outputs in bf16 take the hardware's exp2 and
+// reciprocal (a step each), and for the normal distribution Abramowitz and Stegun's
+// 7.1.26, 1 - erf(x) = (a1 t + .. + a5 t^5) exp(-x^2) with t = 1 / (1 + p x), which
+// is within 1.5e-7: both far below half a step of bf16 of values that are not.
+template <class O, int N>
+__device__ __forceinline__ void activate_all(float* y, int act) {
   if (act == GRACE_ACT_NONE) return;
   if (act == GRACE_ACT_RELU) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = y[e] < 0.f ? 0.f : y[e];
-  } else if (act == GRACE_ACT_GELU) {
+    for (int e = 0; e < N; ++e) y[e] = y[e] < 0.f ? 0.f : y[e];
+  } else if (act == GRACE_ACT_SILU) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = activate(y[e], GRACE_ACT_GELU);
+    for (int e = 0; e < N; ++e) {
+      if constexpr (O::kBytes == 2) y[e] *= __builtin_amdgcn_rcpf(1.f + fast_exp2(-kLog2e * y[e]));
+      else y[e] = activate(y[e], GRACE_ACT_SILU);
+    }
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = activate(y[e], GRACE_ACT_SILU);
+    for (int e = 0; e < N; ++e) {
+      if constexpr (O::kBytes == 2) {
+        const float x = fabsf(y[e]) * 0.70710678118654752f;
+        const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
+        float q = fmaf(t, 1.061405429f, -1.453152027f);
+        q = fmaf(t, q, 1.421413741f);
+        q = fmaf(t, q, -0.284496736f);
+        q = fmaf(t, q, 0.254829592f);
+        const float tail = 0.5f * t * q * fast_exp2(-kLog2e * x * x);   // of the normal distribution
+        y[e] *= y[e] < 0.f ? tail : 1.f - tail;
+      } else {
+        y[e] = activate(y[e], GRACE_ACT_GELU);
+      }
+    }
   }
 }
 
@@ -265,34 +285,33 @@ __device__ __forceinline__ void lds_barrier() {
 
 // Which tile a workgroup takes.  Workgroup i runs on XCD i % 8: each XCD takes a
 // contiguous eighth of the tiles, and these go through groups of 8 row tiles, one
-// column of the group after the other, so that the 64 workgroups an XCD runs at once
-// read 8 row tiles and 8 column tiles through its L2.
+// column of the group after the other, so that what an XCD runs at once is 8 row
+// tiles and a few column tiles, read through its L2.
 struct TileMap {
-  int64_t tiles_r, tiles_n;
-  __device__ bool take(int64_t id, int64_t& tr, int64_t& tn) const {
-    const int64_t all = tiles_r * tiles_n, per = (all + 7) / 8;
-    const int64_t i = id % 8 * per + id / 8;
+  uint32_t tiles_r, tiles_n, all, per;   // per: of an XCD
+  __device__ bool take(uint32_t id, uint32_t& tr, uint32_t& tn) const {
+    const uint32_t i = id % 8 * per + id / 8;
     if (id / 8 >= per || i >= all) return false;
-    const int64_t group = i / (8 * tiles_n), in = i % (8 * tiles_n);
-    const int64_t high = min((int64_t)8, tiles_r - group * 8);
-    tr = group * 8 + in % high;
+    const uint32_t group = i / (8 * tiles_n), in = i - group * 8 * tiles_n;
+    const uint32_t high = min(8u, tiles_r - group * 8);
     tn = in / high;
+    tr = group * 8 + in - tn * high;
     return true;
   }
 };
 
-// Four values from 4-aligned element i of a tensor of O's type.
+// Eight values at element i, a multiple of 8, of a 16-byte aligned tensor.
 template <class O>
-__device__ __forceinline__ void load4(const void* p, int64_t i, float* f) {
-  if constexpr (O::kBytes == 4) {
-    const f32x4 v = *(const f32x4*)((const float*)p + i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = v[e];
-  } else {
-    const u32x2 v = *(const u32x2*)((const uint16_t*)p + i);
-    f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
-    f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
-  }
+__device__ __forceinline__ void load8(const void* p, int64_t i, float* f) {
+  const u32x4* v = (const u32x4*)((const char*)p + i * O::kBytes);
+  Chunk<O>::unpack(v[0], f);
+  if constexpr (O::kBytes == 4) Chunk<O>::unpack(v[1], f + 4);
+}
+template <class O>
+__device__ __forceinline__ void store8(void* p, int64_t i, const float* f) {
+  u32x4* v = (u32x4*)((char*)p + i * O::kBytes);
+  v[0] = Chunk<O>::pack(f);
+  if constexpr (O::kBytes == 4) v[1] = Chunk<O>::pack(f + 4);
 }
 
 // WR x WN waves of RT x NT tiles of 32 x 32: BR rows of x against BN rows of w, in
@@ -318,36 +337,37 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
   constexpr int BR = WR * RT * 32, BN = WN * NT * 32, kRows = BR + BN;
   constexpr int kLoads = kRows / (kTileWaves * 8);         // of 8 rows
   constexpr int kStageBytes = kRows * 128;
-  constexpr int kOutRow = NT * 32 * O::kBytes;             // a wave's output row in LDS
-  constexpr int kOutBytes = VEC ? kTileWaves * 32 * kOutRow : 0;
-  constexpr int kLds = 2 * kStageBytes > kOutBytes ? 2 * kStageBytes : kOutBytes;
-  __shared__ __attribute__((aligned(256))) char lds[kLds];
+  constexpr int kOutBytes = 32 * NT * 128;                 // 32 rows of a wave's sums
+  static_assert(kTileWaves * kOutBytes <= 2 * kStageBytes, "sums fit where the tiles were");
+  __shared__ __attribute__((aligned(256))) char lds[2 * kStageBytes];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, col = lane & 31;
-  int64_t tr, tn;
-  if (!map.take(blockIdx.x, tr, tn)) return;
-  const int64_t r0 = tr * BR;
-  const int32_t n0 = (int32_t)(tn * BN);
 
   // Loads: a wave's instruction covers 8 rows; lane l brings a chunk of row l / 8 to
   // place l % 8, where chunk c of row r lies at place c ^ (r / 2 % 8): 16 rows of one
   // chunk, as a fragment's lanes read them, are on different banks.
   const int64_t pitch = (int64_t)a.K * T::kBytes;
   const int chunk = (lane & 7) ^ ((wave * 4 + (lane >> 4)) & 7);
-  const char* const xb = (const char*)a.x + r0 * pitch;
-  const char* const wb = (const char*)a.w + (int64_t)n0 * pitch;
-  uint32_t off[kLoads];
-#pragma unroll
-  for (int j = 0; j < kLoads; ++j) {
-    const int row = (wave + j * kTileWaves) * 8 + (lane >> 3);
-    const int64_t in = (wave + j * kTileWaves) * 8 < BR ? min((int64_t)row, (int64_t)a.R - 1 - r0)
-                                                        : min((int64_t)row - BR, (int64_t)a.N - 1 - n0);
-    off[j] = (uint32_t)(in * pitch) + chunk * 16;
-  }
-  const int32_t tiles = (int32_t)((pitch + 127) / 128);
+  const int32_t tiles = (int32_t)((pitch + 127) / 128);    // of k
   const int last_chunks = (int)((pitch - (int64_t)(tiles - 1) * 128) / 16);
   const bool beyond = chunk >= last_chunks;                // in the last tile: past k's end
   const uint32_t lds0 = lds_addr(lds);
+  uint32_t tr, tn;
+  if (!map.take(blockIdx.x, tr, tn)) return;
+  const int64_t r0 = (int64_t)tr * BR;
+  const int32_t n0 = (int32_t)(tn * BN);
+  const char* const xb = (const char*)a.x + r0 * pitch;
+  const char* const wb = (const char*)a.w + (int64_t)n0 * pitch;
+  uint32_t off[kLoads];
+  {
+    const int rows = (int)min((int64_t)BR, (int64_t)a.R - r0) - 1, cols = min(BN, a.N - n0) - 1;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int row = (wave + j * kTileWaves) * 8 + (lane >> 3);
+      off[j] = (uint32_t)((wave + j * kTileWaves) * 8 < BR ? min(row, rows) : min(row - BR, cols)) *
+                   (uint32_t)pitch + chunk * 16;
+    }
+  }
   const auto load = [&](int32_t t, int j) {
     // what lies past a row's end reads the row's first chunk of the tile, and is cleared later
     const uint32_t back = t == tiles - 1 && beyond ? chunk * 16 : 0;
@@ -360,7 +380,7 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
     for (int j = part * kPerRow; j < (part + 1) * kPerRow; ++j)
       if (j < kLoads) load(t, j);
   };
-  // Tile t has landed, its end of k is clean, and every wave knows it.
+  // Tile t of k has landed, its end is clean, and every wave knows it.
   const auto hand_over = [&](int32_t t) {
     wait_loads<0>();
     if (t == tiles - 1 && beyond)
@@ -371,10 +391,6 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
   };
 
   f32x16 acc[RT][NT];
-#pragma unroll
-  for (int i = 0; i < RT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) acc[i][j] = f32x16{0};
   const int wr = wave / WN * RT * 32, wn = wave % WN * NT * 32;
   const int swz = col >> 1 & 7;
   const char* const xrow = lds + (wr + col) * 128;
@@ -387,7 +403,7 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
       c[i] = *(const u32x4*)(row + stage * kStageBytes + (((s * 2 + half) * S::kChunks + i) ^ swz) * 16);
     return S::make(c);
   };
-  // tile t; next: there is a tile behind it, more: and one behind that
+  // tile t of k; next: there is a tile behind it, more: and one behind that
   const auto tile = [&](int32_t t, auto next, auto more) {
     const int stage = t & 1;
 #pragma unroll
@@ -415,12 +431,19 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
   };
   struct Yes { constexpr operator bool() const { return true; } };
   struct No { constexpr operator bool() const { return false; } };
+
 #pragma unroll
   for (int j = 0; j < kLoads; ++j) load(0, j);
-  hand_over(0);
   if (tiles > 1)
 #pragma unroll
     for (int i = 0; i < RT; ++i) load_part(1, i);
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x16{0};
+  if (tiles > 1) wait_loads<kPerRow * RT < kLoads ? kPerRow * RT : kLoads>();
+  else hand_over(0);
+  if (tiles > 1) lds_barrier();
 #pragma unroll
   for (int j = 0; j < NT; ++j) fn[0][j] = frag(wrow + j * 32 * 128, 0, 0);
 #pragma unroll
@@ -437,54 +460,53 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
     for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(acc[i][j]));
   lds_barrier();
 
-  // Epilogue in the accumulators' layout: lane l has rows r = l % 32 and, of every 8
-  // columns, 4 (l / 32) .. + 3.
+  // Epilogue.  In the accumulators lane l has row l % 32 and, of every 8 columns, 4 (l /
+  // 32) .. + 3; 32 rows at a time they go through LDS of the wave's own, so that a
+  // lane has 8 columns, the same for all its rows, and rows leave as whole lines.
   if constexpr (VEC) {
-    char* const mine = lds + wave * 32 * kOutRow;
+    constexpr int kRowChunk = NT * 8, kLanes = kRowChunk / 2, kPer = 32 * kLanes / 64;
+    const auto at = [&](int row, int c) {                   // 16 rows of one chunk on different banks
+      const int turn = kRowChunk == 16 ? row : row >> 1;
+      return row * NT * 128 + (c ^ (turn & (kRowChunk - 1))) * 16;
+    };
+    char* const mine = lds + wave * kOutBytes;
+    const int row_in = lane / kLanes, c = lane % kLanes * 2;
+    const int32_t n = n0 + wn + c * 4;
+    const bool in = n < a.N;
+    float ws[8], bias[8], xs[RT][kPer];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ws[e] = 1.f, bias[e] = 0.f;
+    if (a.w_scale && in) load8<F32>(a.w_scale, n, ws);
+    if (a.bias && in) load8<O>(a.bias, n, bias);
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int q = 0; q < kPer; ++q)
+        xs[i][q] = a.x_scale ? a.x_scale[min(r0 + wr + i * 32 + q * (64 / kLanes) + row_in, (int64_t)a.R - 1)] : 1.f;
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
-      const int64_t r = min(r0 + wr + i * 32 + col, (int64_t)a.R - 1);
-      const float xs = a.x_scale ? a.x_scale[r] : 1.f;
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int32_t n = min(n0 + wn + j * 32 + g * 8 + half * 4, a.N - 4);
-          float y[4], v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = acc[i][j][g * 4 + e] * xs;
-          if (a.w_scale) {
-            load4<F32>(a.w_scale, n, v);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] *= v[e];
-          }
-          if (a.bias) {
-            load4<O>(a.bias, n, v);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] += v[e];
-          }
-          activate4(y, a.act);
-          if (a.residual) {
-            load4<O>(a.residual, r * a.N + n, v);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] += v[e];
-          }
-          // 16-byte chunks of a row, swizzled over the rows
-          constexpr int kRowChunk = kOutRow / 16;
-          const int byte = (j * 32 + g * 8 + half * 4) * O::kBytes;
-          char* const to = mine + col * kOutRow + ((byte / 16) ^ (col >> 1 & (kRowChunk - 1))) * 16 + byte % 16;
-          if constexpr (O::kBytes == 4) *(f32x4*)to = f32x4{y[0], y[1], y[2], y[3]};
-          else *(u32x2*)to = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
-        }
-      // whole lines of the wave's 32 rows
-      constexpr int kRowChunk = kOutRow / 16, kPer = 32 * kRowChunk / 64;
+        for (int g = 0; g < 4; ++g)
+          *(f32x4*)(mine + at(col, j * 8 + g * 2 + half)) =
+              f32x4{acc[i][j][g * 4], acc[i][j][g * 4 + 1], acc[i][j][g * 4 + 2], acc[i][j][g * 4 + 3]};
 #pragma unroll
       for (int q = 0; q < kPer; ++q) {
-        const int row = (q * 64 + lane) / kRowChunk, c = lane % kRowChunk;
-        const u32x4 v = *(const u32x4*)(mine + row * kOutRow + (c ^ (row >> 1 & (kRowChunk - 1))) * 16);
+        const int row = q * (64 / kLanes) + row_in;
         const int64_t r = r0 + wr + i * 32 + row;
-        const int32_t n = n0 + wn + c * (16 / O::kBytes);
-        if (r < a.R && n < a.N) *(u32x4*)((char*)a.out + (r * a.N + n) * O::kBytes) = v;
+        float y[8], res[8];
+        *(f32x4*)y = *(const f32x4*)(mine + at(row, c));
+        *(f32x4*)(y + 4) = *(const f32x4*)(mine + at(row, c + 1));
+        if (r >= a.R || !in) continue;
+        if (a.residual) load8<O>(a.residual, r * a.N + n, res);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = fmaf(y[e], xs[i][q] * ws[e], bias[e]);
+        activate_all<O, 8>(y, a.act);
+        if (a.residual)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] += res[e];
+        store8<O>(a.out, r * a.N + n, y);
       }
     }
   } else {
@@ -507,8 +529,10 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
 template <class T, class O, int WR, int WN, int RT, int NT>
 hipError_t run_tile(const LinearArgs& a, hipStream_t stream) {
   constexpr int BR = WR * RT * 32, BN = WN * NT * 32, kThreads = WR * WN * 64;
-  const TileMap map{((int64_t)a.R + BR - 1) / BR, ((int64_t)a.N + BN - 1) / BN};
-  const uint32_t grid = (uint32_t)((map.tiles_r * map.tiles_n + 7) / 8 * 8);
+  const uint32_t tiles_r = (uint32_t)(((int64_t)a.R + BR - 1) / BR), tiles_n = (uint32_t)(((int64_t)a.N + BN - 1) / BN);
+  const uint32_t all = tiles_r * tiles_n, per = (all + 7) / 8;
+  const TileMap map{tiles_r, tiles_n, all, per};
+  const uint32_t grid = 8 * per;
   const uintptr_t any = (uintptr_t)a.out | (uintptr_t)a.bias | (uintptr_t)a.residual | (uintptr_t)a.w_scale;
   if (a.N % 8 == 0 && any % 16 == 0)
     linear_tile_kernel<T, O, WR, WN, RT, NT, true><<<grid, kThreads, 0, stream>>>(a, map);
