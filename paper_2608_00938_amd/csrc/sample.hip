@@ -15,8 +15,8 @@
 //
 // A draw next to a border has to fall as it does by the definition.  Rows in
 // registers are decided with fp32 masses where these lie further from every border
-// than they can be off, and else once more in fp64; the other rows are summed in
-// fp64 throughout.
+// than they can be off, and else once more in fp64; longer rows are summed in fp64
+// throughout.
 #include <float.h>
 #include <math.h>
 
@@ -75,183 +75,481 @@ struct Rules {
   }
 };
 
-// The weight of a key; equal keys weigh the same, and the best key weighs 1.
-__device__ __forceinline__ double weight_of(uint32_t key, uint32_t best, double T) {
-  return key == best ? 1.0 : exp(((double)key_value(key) - (double)key_value(best)) / T);
+// ---------------------------------------------------------------------------
+// One workgroup per row, for rows longer than a wave's registers hold.
+//
+// What each rule keeps is found in a histogram instead of a search over the row:
+// one sweep counts the candidates by the upper half of their bits, which for bf16
+// is their value, with each bin's mass; fp32 bins, and the one bin of the values
+// next to zero, are cut again by their keys where a border falls into them.  A
+// sweep then adds up the kept weights of each wave's piece of the vocabulary, the
+// piece with the drawn token is dealt out again over the waves, and so on down to
+// 512 tokens, which one wave goes through.
+//
+// All sums are fp64, whose exp2 costs a sweep some 90 cycles per wave of tokens; of
+// bf16 only the bins need it.  Candidates whose weight is below 2^-63 are left out:
+// all of a row's together are below 2^-39 of the total, a part that decides nothing
+// but draws with u below 2^-30, which leave none out.
+// ---------------------------------------------------------------------------
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
+
+// 2^x for x <= 0, by the series of exp(f ln 2) on |f| <= 1/2 (to f^11: 6e-15).
+__device__ __forceinline__ double exp2_f64(double x) {
+  const double n = rint(x), y = (x - n) * 0.69314718055994530942;
+  double s = 1.0 / 39916800;
+  s = fma(s, y, 1.0 / 3628800);
+  s = fma(s, y, 1.0 / 362880);
+  s = fma(s, y, 1.0 / 40320);
+  s = fma(s, y, 1.0 / 5040);
+  s = fma(s, y, 1.0 / 720);
+  s = fma(s, y, 1.0 / 120);
+  s = fma(s, y, 1.0 / 24);
+  s = fma(s, y, 1.0 / 6);
+  s = fma(s, y, 0.5);
+  s = fma(s, y, 1.0);
+  s = fma(s, y, 1.0);
+  return ldexp(s, max((int)n, -1100));
 }
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
-
-// Sum over the workgroup, for every thread.
-template <class T>
-__device__ T group_total(T x, T* scratch) {
-  for (int s = 32; s > 0; s >>= 1) x += __shfl_xor(x, s);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = x;
-  __syncthreads();
-  x = scratch[0];
-  for (int w = 1; w < kWaves; ++w) x += scratch[w];
-  return x;
-}
-// Sum of the threads before this one, and of all.
-template <class T>
-__device__ T group_before(T x, T* scratch, T& all) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  T s = x;
-  for (int d = 1; d < 64; d <<= 1) {
-    const T y = __shfl_up(s, d);
-    if (lane >= d) s += y;
+// Bins by value, the largest first: 16 octaves of 128 bins above zero from the one
+// of the row's largest magnitude down, one bin for the smaller values of either
+// sign, 16 octaves below zero.
+struct Bins {
+  static constexpr int kSide = 16 * 128, kCount = 2 * kSide + 1;
+  uint32_t base;                                           // upper half of the least magnitude of a side
+  __device__ explicit Bins(float most) {
+    const int e = (int)(__float_as_uint(most) >> 23 & 255) - 15;
+    base = (uint32_t)max(e, 0) << 7;
   }
-  __syncthreads();
-  if (lane == 63) scratch[wave] = s;
-  __syncthreads();
-  T before = 0;
-  all = 0;
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) before += scratch[w];
-    all += scratch[w];
+  __device__ int of(float x) const {
+    const uint32_t bits = __float_as_uint(x), high = (bits & 0x7fffffffu) >> 16;
+    if (high < base || high == 0) return kSide;            // 0 itself too, where base is 0
+    const int at = (int)min(high - base, (uint32_t)kSide - 1);
+    return bits >> 31 ? kSide + 1 + at : kSide - 1 - at;
   }
-  return before + s - x;
-}
-
-// One workgroup per row, the row read from memory at every step.  Any size.
-template <class T>
-__global__ void __launch_bounds__(kThreads) sample_kernel(SampleArgs a) {
-  __shared__ double sums[kWaves];
-  __shared__ uint32_t counts[kWaves];
-  __shared__ int32_t found[2];
-  const int tid = threadIdx.x;
-  const int64_t r = blockIdx.x;
-  const Rules rules(a, (int32_t)(r / a.M));
-  const int64_t words = (a.V + 31) / 32;
-  const auto key_at = [&](int32_t v) -> uint32_t {
-    if (a.mask && !((a.mask[r * words + v / 32] >> (v % 32)) & 1)) return 0;
-    const float z = logit_at<T>(a, r, v);
-    return z > -INFINITY ? order_key(z) : 0u;              // a NaN is no candidate
-  };
-
-  // best candidate, and the whole row's log-sum-exp
-  uint32_t best = 0;
-  float top = -INFINITY;
-  bool nan = false;
-  for (int32_t v = tid; v < a.V; v += kThreads) {
-    const float z = logit_at<T>(a, r, v);
-    nan |= z != z;
-    top = fmaxf(top, z);
-    best = max(best, key_at(v));
-  }
-  uint32_t nans = nan;
-  nans = group_total(nans, counts);
-  for (int s = 32; s > 0; s >>= 1) {
-    best = max(best, (uint32_t)__shfl_xor((int)best, s));
-    top = fmaxf(top, __shfl_xor(top, s));
-  }
-  __syncthreads();
-  if ((tid & 63) == 0) counts[tid >> 6] = best, sums[tid >> 6] = top;
-  __syncthreads();
-  for (int w = 0; w < kWaves; ++w) best = max(best, counts[w]), top = fmaxf(top, (float)sums[w]);
-  __syncthreads();
-  if (best == 0) {
-    if (tid == 0) a.tokens[r] = -1, a.scores[r] = -INFINITY;
-    return;
-  }
-  double e = 0;
-  for (int32_t v = tid; v < a.V; v += kThreads) e += expf(logit_at<T>(a, r, v) - top);
-  e = group_total(e, sums);
-
-  const double T1 = rules.T > 0 ? rules.T : 1.0;
-  const auto count_from = [&](uint32_t t) {                // candidates of key t and above
-    uint32_t n = 0;
-    for (int32_t v = tid; v < a.V; v += kThreads) n += key_at(v) >= t;
-    return group_total(n, counts);
-  };
-  const auto mass_above = [&](uint32_t t) {                // of keys above t
-    double m = 0;
-    for (int32_t v = tid; v < a.V; v += kThreads) {
-      const uint32_t k = key_at(v);
-      if (k > t) m += weight_of(k, best, T1);
+  // Keys of a bin: [lo, hi).
+  __device__ void keys(int bin, uint32_t& lo, uint32_t& hi) const {
+    const auto up = [&](int at) {                           // the least key of a bin above zero
+      const uint32_t high = base + (uint32_t)at;
+      return 0x80000000u + (max(high, 1u) << 16);
+    };
+    const auto down = [&](int at) {                         // the key past a bin below zero
+      const uint32_t high = base + (uint32_t)at;
+      return 0x80000000u - (max(high, 1u) << 16);
+    };
+    if (bin < kSide) {
+      lo = up(kSide - 1 - bin);
+      hi = bin == 0 ? 0xffffffffu : up(kSide - bin);
+    } else if (bin == kSide) {
+      lo = down(0), hi = up(0);
+    } else {
+      const int at = bin - kSide - 1;
+      hi = down(at);
+      lo = at == kSide - 1 ? 0u : down(at + 1);
     }
-    return group_total(m, sums);
-  };
-
-  // kept: keys above `cut`, and the first `ties` tokens of key `cut`
-  uint32_t cut = 1, ties = 0xffffffffu;
-  if (!(rules.T > 0)) {
-    cut = best, ties = 1;
-  } else if (rules.k < count_from(1)) {
-    uint32_t lo = 1, hi = best;                            // count_from(lo) >= k always
-    while (lo < hi) {
-      const uint32_t mid = lo + (hi - lo + 1) / 2;
-      if (count_from(mid) >= rules.k) lo = mid;
-      else hi = mid - 1;
-    }
-    cut = lo;
-    ties = rules.k - count_from(cut + 1);                  // keys end at that of +inf
   }
-  if (rules.p < 1.0 && rules.T > 0) {
-    // tokens of key cut that are kept (none where no rule has cut yet: key 1 is no logit's)
-    const uint32_t at_cut = min(ties, count_from(cut) - count_from(cut + 1));
-    const double end = at_cut ? at_cut * weight_of(cut, best, T1) : 0.0;
-    const double target = rules.p * (mass_above(cut) + end);
-    // the largest key whose mass, with all above, reaches the target
-    uint32_t lo = cut, hi = best;
-    while (lo < hi) {
-      const uint32_t mid = lo + (hi - lo + 1) / 2;
-      if (mass_above(mid - 1) >= target) lo = mid;
-      else hi = mid - 1;
+};
+
+template <class T, int NT>
+struct RowSampler {
+  static constexpr int kWaves = NT / 64, kParts = 1024;
+  struct Shared {
+    uint32_t count[Bins::kCount];
+    double mass[Bins::kCount];                             // then, of bf16, a bin's weight
+    uint32_t part_count[kParts];
+    double part_mass[kParts];
+    double sums[kWaves];
+    uint32_t counts[kWaves];
+    float tops[kWaves], bests[kWaves];
+    int32_t found;
+    uint32_t found_count;
+    double found_mass;
+  };
+  const SampleArgs& a;
+  Shared& s;
+  const int64_t r;
+  const int tid, lane, wave;
+  const typename T::storage* row;
+  const uint8_t* mask;                                     // the row's filter words, by bytes
+  float best;
+  double scale;                                            // log2(e) / T
+  float least_x;                                           // candidates from here on count
+
+  __device__ RowSampler(const SampleArgs& a_, Shared& s_)
+      : a(a_), s(s_), r(blockIdx.x), tid(threadIdx.x), lane(tid & 63),
+        wave(__builtin_amdgcn_readfirstlane(tid >> 6)),
+        row((const typename T::storage*)a_.logits + r * a_.V),
+        mask(a_.mask ? (const uint8_t*)(a_.mask + r * ((a_.V + 31) / 32)) : nullptr) {}
+
+  // Eight tokens from v on, a multiple of 8: their logits (-inf past the row's end).
+  __device__ void logits(int32_t v, float* x) const {
+    if (v + 8 <= a.V) {
+      u32x4 c = *(const u32x4_any*)(row + v);
+      Chunk<T>::unpack(c, x);
+      if constexpr (T::kBytes == 4) {
+        c = *(const u32x4_any*)(row + v + 4);
+        Chunk<T>::unpack(c, x + 4);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = v + e < a.V ? logit_at<T>(a, r, v + e) : -INFINITY;
     }
-    const double need = (target - mass_above(lo)) / weight_of(lo, best, T1);
-    const uint32_t n = need > 1 ? (uint32_t)fmin(ceil(need), 4294967040.0) : 1;
-    ties = lo == cut ? min(ties, n) : n;
-    cut = lo;
+  }
+  // What is no candidate to -inf: filtered tokens, NaN.
+  __device__ void filter(int32_t v, float* x) const {
+    const uint32_t bits = mask && v < a.V ? mask[v / 8] : 0xff;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = fmaxf(keep_bit(x[e], bits, e), -INFINITY);
+  }
+  // f(v, x) for the eights of this wave's piece of [lo, hi) (lo a multiple of 512), -inf
+  // where there is no candidate; pieces are multiples of 512.
+  __device__ static int32_t piece(int32_t lo, int32_t hi) {
+    return ((hi - lo + kWaves - 1) / kWaves + 511) / 512 * 512;
+  }
+  template <class F>
+  __device__ void sweep(int32_t lo, int32_t hi, F f) const {
+    const int32_t n = piece(lo, hi), from = lo + wave * n, to = min(hi, from + n);
+    for (int32_t v = from + lane * 8; v - lane * 8 < to; v += 512) {
+      float x[8];
+      logits(v, x);
+      filter(v, x);
+      f(v, x);
+    }
+  }
+  __device__ double weight(float x) const {
+    return x == best ? 1.0 : exp2_f64(((double)x - (double)best) * scale);
   }
 
-  // kept weights in vocabulary order: their total, then the draw
-  uint32_t seen = 0;                                       // tokens of key cut so far
-  const auto kept_weight = [&](int32_t base) {
-    const int32_t v = base + tid;
-    const uint32_t k = v < a.V ? key_at(v) : 0;
-    uint32_t all;
-    const uint32_t rank = seen + group_before((uint32_t)(k == cut), counts, all);
-    seen += all;
-    if (k < cut || k == 0 || (k == cut && rank >= ties)) return 0.0;
-    const double w = weight_of(k, best, T1);
-    return k == best || w >= rules.least ? w : 0.0;
-  };
-  double total = 0;
-  for (int32_t base = 0; base < a.V; base += kThreads) total += group_total(kept_weight(base), sums);
-  const float u = fminf(fmaxf(a.uniform[r], 0.f), kMostUniform);   // a NaN is 0
-  const double goal = (double)u * total;
-  if (tid == 0) found[0] = 0x7fffffff, found[1] = -1;
-  __syncthreads();
-  seen = 0;
-  double before = 0;
-  for (int32_t base = 0; base < a.V; base += kThreads) {
-    const double w = kept_weight(base);
-    double all;
-    const double upto = before + group_before(w, sums, all) + w;
-    if (w > 0) {
-      if (upto > goal) atomicMin(&found[0], base + tid);
-      atomicMax(&found[1], base + tid);
-    }
-    before += all;
+  // Sum over the waves of what each wave has, for every thread.
+  template <class V>
+  __device__ V over_waves(V x, V* scratch) {
     __syncthreads();
-    if (found[0] != 0x7fffffff) break;
+    if (lane == 0) scratch[wave] = x;
+    __syncthreads();
+    V all = 0;
+    for (int w = 0; w < kWaves; ++w) all += scratch[w];
+    return all;
   }
-  if (tid == 0) {
-    const int32_t token = found[0] != 0x7fffffff ? found[0] : found[1];
-    const float prev = a.prev ? a.prev[r] : 0.f;
-    a.tokens[r] = token;
-    a.scores[r] = nans ? NAN : prev + (float)((double)logit_at<T>(a, r, token) - (double)top - log(e));
+  template <class V>
+  __device__ static V lanes_total(V x) {
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    return x;
   }
+  template <class V>
+  __device__ static V lanes_upto(V x) {
+    for (int d = 1; d < 64; d <<= 1) {
+      const V y = __shfl_up(x, d);
+      if ((int)(threadIdx.x & 63) >= d) x += y;
+    }
+    return x;
+  }
+
+  // In a histogram of n bins: the first bin with which the count reaches n_goal (by =
+  // 0) or the mass m_goal (by = 1), and what lies before it; -1 if none does.
+  __device__ int locate(const uint32_t* count, const double* mass, int n, int by, uint32_t n_goal,
+                        double m_goal, uint32_t& n_before, double& m_before) {
+    const int each = (n + NT - 1) / NT, lo = min(tid * each, n), hi = min(lo + each, n);
+    uint32_t c = 0;
+    double m = 0;
+    for (int i = lo; i < hi; ++i) c += count[i], m += mass[i];
+    const uint32_t cu = lanes_upto(c);
+    const double mu = lanes_upto(m);
+    __syncthreads();
+    if (lane == 63) s.counts[wave] = cu, s.sums[wave] = mu;
+    if (tid == 0) s.found = -1;
+    __syncthreads();
+    uint32_t cb = cu - c;
+    double mb = 0;
+    for (int w = 0; w < wave; ++w) cb += s.counts[w], mb += s.sums[w];
+    // a lane's mass before is the sum that the lane below ends with, so that the lanes agree
+    const double below = __shfl_up(mu, 1);
+    const double end = mb + mu;
+    mb += lane ? below : 0.0;
+    const bool here = by ? mb < m_goal && end >= m_goal : cb < n_goal && cb + c >= n_goal;
+    if (here) {                                            // rounding aside one of its bins; else its last
+      for (int i = lo; i < hi; ++i) {
+        if (!count[i]) continue;
+        s.found = i, s.found_count = cb, s.found_mass = mb;
+        cb += count[i], mb += mass[i];
+        if (by ? mb >= m_goal : cb >= n_goal) break;
+      }
+    }
+    __syncthreads();
+    n_before = s.found_count, m_before = s.found_mass;
+    const int found = s.found;
+    __syncthreads();
+    return found;
+  }
+
+  // Narrows the keys [lo, hi), which the border falls into, to one key or one token;
+  // n_before, m_before: candidates and mass above hi.  n_at: candidates left in [lo, hi).
+  __device__ void narrow(uint32_t& lo, uint32_t& hi, int by, uint32_t n_goal, double m_goal,
+                         uint32_t& n_before, double& m_before, uint32_t& n_at) {
+    while (hi - lo > 1 && n_at > 1) {
+      const int shift = max(0, 22 - __builtin_clz(hi - lo - 1));   // (hi - lo - 1) >> shift < 1024
+      for (int i = tid; i < kParts; i += NT) s.part_count[i] = 0, s.part_mass[i] = 0;
+      __syncthreads();
+      sweep(0, a.V, [&](int32_t, const float* x) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t k = order_key(x[e]);
+          if (x[e] >= least_x && x[e] > -INFINITY && k >= lo && k < hi) {
+            const uint32_t i = (hi - 1 - k) >> shift;
+            atomicAdd(&s.part_count[i], 1u);
+            if (by) unsafeAtomicAdd(&s.part_mass[i], weight(x[e]));
+          }
+        }
+      });
+      __syncthreads();
+      uint32_t nb;
+      double mb;
+      int i = locate(s.part_count, s.part_mass, kParts, by, n_goal - n_before, m_goal - m_before, nb, mb);
+      if (i < 0) {                                         // rounding alone: the last of them
+        for (i = kParts - 1; i > 0 && !s.part_count[i]; --i) {}
+        nb = 0, mb = 0;
+        for (int j = 0; j < i; ++j) nb += s.part_count[j], mb += s.part_mass[j];
+      }
+      n_before += nb, m_before += mb, n_at = s.part_count[i];
+      const uint32_t end = hi - ((uint32_t)i << shift), width = 1u << shift;
+      lo = end - lo > width ? end - width : lo;
+      hi = end;
+      __syncthreads();
+    }
+  }
+
+  __device__ void run() {
+    const Rules rules(a, (int32_t)(r / a.M));
+    // best candidate and largest logit
+    float top = -INFINITY, most = -INFINITY;
+    {
+      const int32_t n = piece(0, a.V), from = wave * n, to = min(a.V, from + n);
+      for (int32_t v = from + lane * 8; v - lane * 8 < to; v += 512) {
+        float x[8];
+        logits(v, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e]);
+        filter(v, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, x[e]);
+      }
+      top = wave_max(top), most = wave_max(most);
+      if (lane == 0) s.tops[wave] = top, s.bests[wave] = most;
+      for (int i = tid; i < Bins::kCount; i += NT) s.count[i] = 0, s.mass[i] = 0;
+      __syncthreads();
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s.tops[w]), most = fmaxf(most, s.bests[w]);
+      best = most;
+    }
+    if (!(best > -INFINITY)) {
+      if (tid == 0) a.tokens[r] = -1, a.scores[r] = -INFINITY;
+      return;
+    }
+    const float u = fminf(fmaxf(a.uniform[r], 0.f), kMostUniform);   // a NaN is 0
+    const bool greedy = !(rules.T > 0);
+    const double temp = greedy ? 1.0 : rules.T;
+    scale = 1.4426950408889634 / temp;
+    least_x = greedy ? best : (float)((double)best - (u < 0x1p-30f ? 1100 : 63) * 0.6931471805599453 * temp);
+    const Bins bins(fmaxf(fabsf(best), least_x > -FLT_MAX ? fabsf(least_x) : FLT_MAX));
+    const bool cuts = !greedy && (rules.k < (uint32_t)a.V || rules.p < 1.0);
+
+    // the row's sum of exp, and the histogram
+    float e1 = 0;
+    {
+      const int32_t n = piece(0, a.V), from = wave * n, to = min(a.V, from + n);
+      for (int32_t v = from + lane * 8; v - lane * 8 < to; v += 512) {
+        float x[8];
+        logits(v, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) e1 += fast_exp2((x[e] - top) * kLog2e);   // a NaN or +inf makes it NaN
+        if (!cuts) continue;
+        filter(v, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (x[e] >= least_x && x[e] > -INFINITY) {
+            const int b = bins.of(x[e]);
+            atomicAdd(&s.count[b], 1u);
+            if (kMasses || b == Bins::kSide) unsafeAtomicAdd(&s.mass[b], weight(x[e]));
+          }
+      }
+    }
+    const float log_sum = logf((float)over_waves((double)wave_sum(e1), s.sums));
+
+    // kept: values above cut, and the first `ties` tokens of value cut
+    float cut = greedy ? best : -INFINITY;
+    uint32_t ties = greedy ? 1u : 0xffffffffu;
+    if (cuts) {
+      if (!kMasses) {                                    // a bin of bf16 is one value
+        for (int i = tid; i < Bins::kCount; i += NT)
+          if (s.count[i] && i != Bins::kSide) {
+            uint32_t lo, hi;
+            bins.keys(i, lo, hi);
+            s.mass[i] = s.count[i] * weight(bf16_of_keys(lo, hi));
+          }
+        __syncthreads();
+      }
+      uint32_t lo = 0, hi = 0, n_before, n_at;
+      double m_before, total;
+      const auto border = [&](int by, uint32_t n_goal, double m_goal) {
+        const int bin = locate(s.count, s.mass, Bins::kCount, by, n_goal, m_goal, n_before, m_before);
+        if (bin < 0) return false;
+        n_at = s.count[bin];
+        bins.keys(bin, lo, hi);
+        if (kMasses || bin == Bins::kSide) narrow(lo, hi, by, n_goal, m_goal, n_before, m_before, n_at);
+        else lo = order_key(bf16_of_keys(lo, hi));
+        return true;
+      };
+      total = -1;
+      if (border(0, rules.k, 0)) {
+        cut = key_value(lo);
+        ties = rules.k - n_before;
+        if (n_at <= ties) ties = 0xffffffffu;              // all of them: no rank to keep
+      }
+      if (rules.p < 1.0) {
+        // the mass that top-k keeps
+        double m = 0;
+        uint32_t n = 0;
+        if (cut > -INFINITY) {
+          sweep(0, a.V, [&](int32_t, const float* x) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              if (x[e] > cut) m += weight(x[e]);
+              n += x[e] == cut;
+            }
+          });
+          m = over_waves(lanes_total(m), s.sums);
+          n = over_waves(lanes_total(n), s.counts);
+          total = m + min(ties, n) * weight(cut);
+        } else {
+          for (int i = tid; i < Bins::kCount; i += NT) m += s.mass[i];
+          total = over_waves(lanes_total(m), s.sums);
+        }
+        const double target = rules.p * total;
+        if (!(target > 0)) {
+          cut = best, ties = 1;
+        } else if (border(1, 0, target)) {
+          const float at = key_value(lo);
+          if (n_at == 1 && hi - lo > 1) {
+            // one token between the keys: it reaches the target
+            if (at > cut) cut = at, ties = 0xffffffffu;
+          } else {
+            const double need = ceil((target - m_before) / weight(at));
+            const uint32_t first = need > 1 ? (uint32_t)fmin(need, 4294967040.0) : 1u;
+            ties = at == cut ? min(ties, first) : first;
+            cut = at;
+          }
+        }
+      }
+    }
+
+    // The draw: [lo, hi) of the vocabulary, `before` the kept mass below it, `seen` the
+    // tokens of value cut below it.
+    const double least = rules.least, w_cut = cut > -INFINITY ? weight(cut) : 0.0;
+    const bool ranked = ties != 0xffffffffu;
+    const double w_tie = w_cut >= least || cut == best ? w_cut : 0.0;
+    const auto kept = [&](float x) {                       // the weight of what is above the cut
+      if (!(ranked ? x > cut : x >= cut) || !(x >= least_x) || !(x > -INFINITY)) return 0.0;
+      const double w = weight(x);
+      return w >= least || x == best ? w : 0.0;
+    };
+    int32_t lo = 0, hi = a.V;
+    double before = 0, goal = -1;
+    uint32_t seen = 0;
+    while (hi - lo > 512 || goal < 0) {
+      double m = 0;
+      uint32_t n = 0;
+      sweep(lo, hi, [&](int32_t, const float* x) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          m += kept(x[e]);
+          n += ranked && x[e] == cut;
+        }
+      });
+      m = lanes_total(m), n = lanes_total(n);
+      __syncthreads();
+      if (lane == 0) s.sums[wave] = m, s.counts[wave] = n;
+      __syncthreads();
+      const auto of_wave = [&](int w, uint32_t below) {
+        const uint32_t left = ties > below ? ties - below : 0;
+        return s.sums[w] + (ranked ? min(left, s.counts[w]) * w_tie : 0.0);
+      };
+      if (goal < 0) {
+        double all = 0;
+        uint32_t below = 0;
+        for (int w = 0; w < kWaves; ++w) all += of_wave(w, below), below += s.counts[w];
+        goal = (double)u * all;
+      }
+      // the first piece that the running sum passes the goal in; the sums' rounding
+      // aside there is one, and else it is the last with anything in it
+      const int32_t size = piece(lo, hi);
+      int pick = -1;
+      double pick_before = 0, run = before;
+      uint32_t pick_seen = 0, run_seen = seen;
+      for (int w = 0; w < kWaves; ++w) {
+        const double mine = of_wave(w, run_seen);
+        if (mine > 0) {
+          pick = w, pick_before = run, pick_seen = run_seen;
+          if (run + mine > goal) break;
+        }
+        run += mine, run_seen += s.counts[w];
+      }
+      lo += pick * size;
+      hi = min(hi, lo + size);
+      before = pick_before, seen = pick_seen;
+      __syncthreads();
+    }
+    if (wave > 0) return;
+    float x[8];
+    const int32_t v0 = lo + lane * 8;
+    logits(v0, x);
+    filter(v0, x);
+    uint32_t n = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) n += ranked && x[e] == cut;
+    uint32_t rank = seen + lanes_upto(n) - n;
+    double w[8], sum = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      w[e] = v0 + e < hi ? kept(x[e]) : 0.0;
+      if (ranked && x[e] == cut && v0 + e < hi) w[e] = rank++ < ties ? w_tie : 0.0;
+      sum += w[e];
+    }
+    const double upto = lanes_upto(sum);
+    const double below = __shfl_up(upto, 1);               // by every lane: an idle one has no value
+    double run = before + (lane ? below : 0.0);
+    int32_t first = 0x7fffffff, last = -1;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      run += w[e];
+      if (w[e] > 0) {
+        last = v0 + e;
+        if (run > goal && first == 0x7fffffff) first = v0 + e;
+      }
+    }
+    for (int d = 32; d > 0; d >>= 1) first = min(first, __shfl_xor(first, d)), last = max(last, __shfl_xor(last, d));
+    if (lane == 0) {
+      const int32_t token = first != 0x7fffffff ? first : last;
+      const float prev = a.prev ? a.prev[r] : 0.f;
+      a.tokens[r] = token;
+      a.scores[r] = prev + (logit_at<T>(a, r, token) - top - log_sum);
+    }
+  }
+  // whether a bin holds different values, whose mass its tokens add up
+  static constexpr bool kMasses = T::kBytes == 4;
+  // the one bf16 value among the keys [lo, hi) of a bin
+  __device__ static float bf16_of_keys(uint32_t lo, uint32_t hi) {
+    return lo >> 31 ? key_value(lo) : key_value(hi - 1);
+  }
+};
+
+template <class T, int NT>
+__global__ void __launch_bounds__(NT) sample_row_kernel(SampleArgs a) {
+  __shared__ typename RowSampler<T, NT>::Shared shared;
+  RowSampler<T, NT>(a, shared).run();
 }
 
 // ---------------------------------------------------------------------------
 // One wave per row, the row in registers: rows of up to 512 * NCH tokens, lane l
 // holding 8 consecutive tokens of every 512.
 // ---------------------------------------------------------------------------
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
-
 __device__ __forceinline__ double wave_total(double x) {
   for (int s = 32; s > 0; s >>= 1) x += __shfl_xor(x, s);
   return x;
@@ -542,7 +840,8 @@ hipError_t run(const SampleArgs& a, hipStream_t stream) {
   if (a.V <= 512) sample_wave_kernel<T, 1><<<waves, 256, 0, stream>>>(a);
   else if (a.V <= 1024) sample_wave_kernel<T, 2><<<waves, 256, 0, stream>>>(a);
   else if (a.V <= 2048) sample_wave_kernel<T, 4><<<waves, 256, 0, stream>>>(a);
-  else sample_kernel<T><<<a.R, kThreads, 0, stream>>>(a);
+  else if (a.V <= 8192) sample_row_kernel<T, 256><<<a.R, 256, 0, stream>>>(a);
+  else sample_row_kernel<T, 1024><<<a.R, 1024, 0, stream>>>(a);
   return hipGetLastError();
 }
 
