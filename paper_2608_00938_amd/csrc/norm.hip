@@ -48,44 +48,63 @@ __device__ __forceinline__ uint32_t row_max(uint32_t x, uint32_t* scratch) {
   return x;
 }
 
-// E consecutive elements at p as fp32 (E = 1, or a 16-byte chunk).
-template <class T, int E>
-__device__ __forceinline__ void load_elems(const typename T::storage* p, float* f) {
-  if constexpr (E == 1) {
-    f[0] = T::kBytes == 4 ? *(const float*)p : bf16_bits_to_f32(*(const uint16_t*)p);
+// Loads and stores at any address: the hardware takes them off their alignment.
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
+
+// E (a 16-byte chunk) elements from element `at` of a row of D as fp32, those past
+// its end 0.
+template <class T>
+__device__ __forceinline__ void load_elems(const typename T::storage* row, int32_t at, int32_t D, float* f) {
+  constexpr int E = Chunk<T>::kElems;
+  if (at + E <= D) {
+    const u32x4 c = *(const u32x4_any*)(row + at);
+    Chunk<T>::unpack(c, f);
   } else {
-    Chunk<T>::unpack(*(const u32x4*)p, f);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      f[e] = 0.f;
+      if (at + e < D) {
+        if constexpr (T::kBytes == 4) f[e] = row[at + e];
+        else f[e] = bf16_bits_to_f32(row[at + e]);
+      }
+    }
   }
 }
 
-// E elements rounded to type code `to` at element `at` of out.
-template <int E>
-__device__ __forceinline__ void store_elems(void* out, int64_t at, const float* f, int to) {
-  if (to == GRACE_F32) {
-    float* o = (float*)out + at;
-    if constexpr (E == 1) *o = f[0];
-    else
+// The same back, rounded to type TO.
+template <int TO, int E>
+__device__ __forceinline__ void store_elems(void* row, int32_t at, int32_t D, const float* f) {
+  if (at + E <= D) {
 #pragma unroll
-      for (int e = 0; e < E; e += 4) *(f32x4*)(o + e) = f32x4{f[e], f[e + 1], f[e + 2], f[e + 3]};
-  } else if (to == GRACE_BF16) {
-    uint16_t* o = (uint16_t*)out + at;
-    if constexpr (E == 1) *o = (uint16_t)pack_bf16x2(f[0], 0.f);
-    else
-#pragma unroll
-      for (int e = 0; e < E; e += 4)
-        *(u32x2*)(o + e) = u32x2{pack_bf16x2(f[e], f[e + 1]), pack_bf16x2(f[e + 2], f[e + 3])};
+    for (int e = 0; e < E; e += 4) {
+      if constexpr (TO == GRACE_F32)
+        *(u32x4_any*)((float*)row + at + e) = u32x4{__float_as_uint(f[e]), __float_as_uint(f[e + 1]),
+                                                    __float_as_uint(f[e + 2]), __float_as_uint(f[e + 3])};
+      else if constexpr (TO == GRACE_E4M3 && E == 4)
+        *(u32_any*)((uint8_t*)row + at) = pack_e4m3x4(f[0], f[1], f[2], f[3]);
+      else if constexpr (TO == GRACE_BF16 && E == 4)
+        *(u32x2_any*)((uint16_t*)row + at) = u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
+    }
+    if constexpr (TO == GRACE_BF16 && E == 8) *(u32x4_any*)((uint16_t*)row + at) = Chunk<BF16>::pack(f);
+    if constexpr (TO == GRACE_E4M3 && E == 8)
+      *(u32x2_any*)((uint8_t*)row + at) = u32x2{pack_e4m3x4(f[0], f[1], f[2], f[3]),
+                                                pack_e4m3x4(f[4], f[5], f[6], f[7])};
   } else {
-    uint8_t* o = (uint8_t*)out + at;
-    if constexpr (E == 1) *o = (uint8_t)pack_e4m3x4(f[0], 0.f, 0.f, 0.f);
-    else
 #pragma unroll
-      for (int e = 0; e < E; e += 4)
-        *(uint32_t*)(o + e) = pack_e4m3x4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+    for (int e = 0; e < E; ++e)
+      if (at + e < D) {
+        if constexpr (TO == GRACE_F32) ((float*)row)[at + e] = f[e];
+        else if constexpr (TO == GRACE_BF16) ((uint16_t*)row)[at + e] = (uint16_t)pack_bf16x2(f[e], 0.f);
+        else ((uint8_t*)row)[at + e] = (uint8_t)pack_e4m3x4(f[e], 0.f, 0.f, 0.f);
+      }
   }
 }
 
-// NT lanes own a row; lane i takes the groups of E elements at (i + j * NT) * E.
-template <class T, int NT, int E, int NG, int OUT>
+// NT lanes own a row; lane i takes the 16-byte groups of E elements at (i + j * NT) * E.
+// Rows and tensors may start anywhere; a row's last group may be short.
+template <class T, int NT, int NG, int OUT>
 __global__ void __launch_bounds__(NT == 64 ? 256 : NT)
 rms_norm_kernel(const typename T::storage* x, const typename T::storage* residual,
                 const typename T::storage* weight, typename T::storage* sum, void* out,
@@ -95,15 +114,18 @@ rms_norm_kernel(const typename T::storage* x, const typename T::storage* residua
   const int lane = threadIdx.x % NT;
   const int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / NT;
   if (r >= R) return;                          // whole waves of a one-wave row only
+  constexpr int E = Chunk<T>::kElems;
+  constexpr int kOutBytes = OUT == GRACE_F32 ? 4 : (OUT == GRACE_BF16 ? 2 : 1);
   const int64_t row = r * D;
   float h[NG][E], w[NG][E];
   // everything is read before the first write: sum may be x or residual itself
 #pragma unroll
   for (int j = 0; j < NG; ++j) {
     const int32_t at = (lane + j * NT) * E;
+    if (at < D) load_elems<T>(x + row, at, D, h[j]);
+    else
 #pragma unroll
-    for (int e = 0; e < E; ++e) h[j][e] = 0.f;
-    if (at < D) load_elems<T, E>(x + row + at, h[j]);
+      for (int e = 0; e < E; ++e) h[j][e] = 0.f;
   }
   if (residual) {
 #pragma unroll
@@ -111,7 +133,7 @@ rms_norm_kernel(const typename T::storage* x, const typename T::storage* residua
       const int32_t at = (lane + j * NT) * E;
       if (at < D) {
         float a[E];
-        load_elems<T, E>(residual + row + at, a);
+        load_elems<T>(residual + row, at, D, a);
 #pragma unroll
         for (int e = 0; e < E; ++e) h[j][e] += a[e];
       }
@@ -120,13 +142,13 @@ rms_norm_kernel(const typename T::storage* x, const typename T::storage* residua
 #pragma unroll
   for (int j = 0; j < NG; ++j) {
     const int32_t at = (lane + j * NT) * E;
-    if (at < D) load_elems<T, E>(weight + at, w[j]);
+    if (at < D) load_elems<T>(weight, at, D, w[j]);
   }
   float ss = 0.f;
 #pragma unroll
   for (int j = 0; j < NG; ++j) {
     const int32_t at = (lane + j * NT) * E;
-    if (sum && at < D) store_elems<E>(sum, row + at, h[j], T::kBytes == 4 ? GRACE_F32 : GRACE_BF16);
+    if (sum && at < D) store_elems<T::kBytes == 4 ? GRACE_F32 : GRACE_BF16, E>(sum + row, at, D, h[j]);
 #pragma unroll
     for (int e = 0; e < E; ++e) ss = fmaf(h[j][e], h[j][e], ss);
   }
@@ -155,7 +177,7 @@ rms_norm_kernel(const typename T::storage* x, const typename T::storage* residua
 #pragma unroll
   for (int j = 0; j < NG; ++j) {
     const int32_t at = (lane + j * NT) * E;
-    if (at < D) store_elems<E>(out, row + at, h[j], OUT);
+    if (at < D) store_elems<OUT, E>((char*)out + row * kOutBytes, at, D, h[j]);
   }
 }
 
@@ -168,56 +190,40 @@ struct NormArgs {
   hipStream_t stream;
 };
 
-template <class T, int NT, int E, int NG, int OUT>
+template <class T, int NT, int NG, int OUT>
 hipError_t run(const NormArgs& a) {
   using S = typename T::storage;
   const int64_t rows = NT == 64 ? 4 : 1;
-  rms_norm_kernel<T, NT, E, NG, OUT><<<(uint32_t)((a.R + rows - 1) / rows), NT == 64 ? 256 : NT, 0, a.stream>>>(
+  rms_norm_kernel<T, NT, NG, OUT><<<(uint32_t)((a.R + rows - 1) / rows), NT == 64 ? 256 : NT, 0, a.stream>>>(
       (const S*)a.x, (const S*)a.residual, (const S*)a.weight, (S*)a.sum, a.out, a.scale, a.R, a.D,
       a.eps);
   return hipGetLastError();
 }
 
 // Groups per lane, the least power of two that holds the row.
-template <class T, int NT, int E, int OUT>
+template <class T, int NT, int OUT>
 hipError_t pick_groups(const NormArgs& a) {
-  constexpr int kMost = kPerLane / E;
+  constexpr int E = Chunk<T>::kElems, kMost = kPerLane / E;
   const int32_t need = (a.D + NT * E - 1) / (NT * E);
-  if constexpr (kMost >= 32) {
-    if (need > 16) return run<T, NT, E, 32, OUT>(a);
-  }
-  if constexpr (kMost >= 16) {
-    if (need > 8) return run<T, NT, E, 16, OUT>(a);
-  }
   if constexpr (kMost >= 8) {
-    if (need > 4) return run<T, NT, E, 8, OUT>(a);
+    if (need > 4) return run<T, NT, 8, OUT>(a);
   }
-  if (need > 2) return run<T, NT, E, 4, OUT>(a);
-  return need > 1 ? run<T, NT, E, 2, OUT>(a) : run<T, NT, E, 1, OUT>(a);
-}
-
-template <class T, int E, int OUT>
-hipError_t pick_lanes(const NormArgs& a) {
-  if (a.D <= 64 * kPerLane) return pick_groups<T, 64, E, OUT>(a);
-  if (a.D <= 256 * kPerLane) return pick_groups<T, 256, E, OUT>(a);
-  return pick_groups<T, 1024, E, OUT>(a);
+  if (need > 2) return run<T, NT, 4, OUT>(a);
+  return need > 1 ? run<T, NT, 2, OUT>(a) : run<T, NT, 1, OUT>(a);
 }
 
 template <class T, int OUT>
-hipError_t pick_width(const NormArgs& a) {
-  // 16-byte chunks where every row of every tensor starts on one
-  constexpr int E = Chunk<T>::kElems;
-  const uintptr_t any = (uintptr_t)a.x | (uintptr_t)a.residual | (uintptr_t)a.weight |
-                        (uintptr_t)a.sum | (uintptr_t)a.out;
-  if (a.D % E == 0 && (any & 15) == 0) return pick_lanes<T, E, OUT>(a);
-  return pick_lanes<T, 1, OUT>(a);
+hipError_t pick_lanes(const NormArgs& a) {
+  if (a.D <= 64 * kPerLane) return pick_groups<T, 64, OUT>(a);
+  if (a.D <= 256 * kPerLane) return pick_groups<T, 256, OUT>(a);
+  return pick_groups<T, 1024, OUT>(a);
 }
 
 template <class T>
 hipError_t pick_out(const NormArgs& a, int32_t out_dtype) {
-  if (out_dtype == GRACE_F32) return pick_width<T, GRACE_F32>(a);
-  if (out_dtype == GRACE_BF16) return pick_width<T, GRACE_BF16>(a);
-  return pick_width<T, GRACE_E4M3>(a);
+  if (out_dtype == GRACE_F32) return pick_lanes<T, GRACE_F32>(a);
+  if (out_dtype == GRACE_BF16) return pick_lanes<T, GRACE_BF16>(a);
+  return pick_lanes<T, GRACE_E4M3>(a);
 }
 
 }  // namespace

@@ -442,30 +442,36 @@ def grace_trie_advance(index: GtmIndex, node_prev, parents, tokens, B: int, M_pr
     return node_next
 
 
-def _expect(name: str, t, shape, dtype, device):
-    """t is a contiguous tensor of this shape, type and device (or None): a call
-    that passes sizes and raw pointers has no other check of them."""
-    if t is None:
+def _expect(name: str, t, shape, dtype, index: int):
+    """t is a contiguous tensor of this shape and type on GPU ``index`` (or None): a
+    call that passes sizes and raw pointers has no other check of them.  (One test
+    that passes costs 0.3 us; the six of a norm are a third of the call.)"""
+    if t is None or (t.dtype is dtype and t.shape == shape and t.get_device() == index
+                     and t.is_contiguous()):
         return
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
     if t.dtype != dtype:
         raise TypeError(f"{name} is {t.dtype}, not {dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not {device}")
-    if not t.is_contiguous():
-        raise ValueError("tensors passed to libgrace must be contiguous")
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, not on the GPU of the first argument")
+    raise ValueError("tensors passed to libgrace must be contiguous")
+
+
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _call(fn: str, like: torch.Tensor, *args):
     """Call an entry point on the current stream of ``like``'s GPU, with that GPU
     current (a kernel is launched on the current GPU)."""
     stream = _stream(like)
-    if like.get_device() == torch.cuda.current_device():
-        _check(getattr(library(), fn)(*args, stream), fn)
+    if like.get_device() == _get_device():
+        st = getattr(library(), fn)(*args, stream)
     else:
         with torch.cuda.device(like.device):
-            _check(getattr(library(), fn)(*args, stream), fn)
+            st = getattr(library(), fn)(*args, stream)
+    if st != GRACE_OK:
+        raise GraceError(st, fn)
 
 
 def grace_sample_workspace_bytes(B: int, M: int, V: int) -> int:
@@ -483,7 +489,7 @@ def grace_sample(logits, uniform, B: int, M: int, temperature=None, top_k=None, 
     device uint8 tensor of at least grace_sample_workspace_bytes(B, M, V) bytes
     (allocated here when not given and needed)."""
     R, V = logits.shape
-    dev, f32, i32 = logits.device, torch.float32, torch.int32
+    dev, f32, i32 = logits.get_device(), torch.float32, torch.int32
     code = _dtype_code(logits)
     if R != B * M:
         raise ValueError(f"logits has {R} rows, not {B} * {M}")
@@ -496,16 +502,16 @@ def grace_sample(logits, uniform, B: int, M: int, temperature=None, top_k=None, 
     _expect("top_p", top_p, (B,), f32, dev)
     _expect("min_p", min_p, (B,), f32, dev)
     if tokens is None:
-        tokens = torch.empty((R,), dtype=i32, device=dev)
+        tokens = torch.empty((R,), dtype=i32, device=logits.device)
     if scores is None:
-        scores = torch.empty((R,), dtype=f32, device=dev)
+        scores = torch.empty((R,), dtype=f32, device=logits.device)
     _expect("tokens", tokens, (R,), i32, dev)
     _expect("scores", scores, (R,), f32, dev)
     size = 0
     if workspace is None:
         need = grace_sample_workspace_bytes(B, M, V)
         if need > 0:
-            workspace = torch.empty((need,), dtype=torch.uint8, device=dev)
+            workspace = torch.empty((need,), dtype=torch.uint8, device=logits.device)
             size = need
     else:
         _expect("workspace", workspace, workspace.shape, workspace.dtype, dev)
@@ -528,16 +534,16 @@ def grace_rms_norm(x, weight, eps: float = 1e-6, residual=None, sum_out=None, ou
     given, else x's; float32, bfloat16 or float8_e4m3fn.  Returns out, or
     (out, out_scale fp32 [R]) in 8 bits: out * out_scale[:, None] stands for the norm."""
     R, D = x.shape
-    dev, dtype = x.device, x.dtype
+    dev, dtype = x.get_device(), x.dtype
     if out_dtype is None:
         out_dtype = dtype if out is None else out.dtype
     code, out_code = _dtype_code(x), _ANY_DTYPE_CODE.get(out_dtype)
     if out_code is None:
         raise TypeError(f"unsupported dtype {out_dtype}")
     if out is None:
-        out = torch.empty(x.shape, dtype=out_dtype, device=dev)
+        out = torch.empty(x.shape, dtype=out_dtype, device=x.device)
     if out_code == GRACE_E4M3 and out_scale is None:
-        out_scale = torch.empty((R,), dtype=torch.float32, device=dev)
+        out_scale = torch.empty((R,), dtype=torch.float32, device=x.device)
     _expect("x", x, x.shape, dtype, dev)
     _expect("weight", weight, (D,), dtype, dev)
     _expect("residual", residual, x.shape, dtype, dev)
@@ -561,7 +567,7 @@ def grace_linear(x, w, bias=None, act: str = "none", residual=None, x_scale=None
     bf16 for 8-bit inputs.  ``act``: a name in ACTIVATIONS.  ``residual`` may be out
     itself.  Returns out [R, N]."""
     (R, K), N = x.shape, w.shape[0]
-    dev, dtype = x.device, x.dtype
+    dev, dtype = x.get_device(), x.dtype
     code = _ANY_DTYPE_CODE.get(dtype)
     if code is None:
         raise TypeError(f"unsupported dtype {dtype}")
@@ -573,7 +579,7 @@ def grace_linear(x, w, bias=None, act: str = "none", residual=None, x_scale=None
     if act not in ACTIVATIONS:
         raise ValueError(f"unknown activation {act!r}")
     if out is None:
-        out = torch.empty((R, N), dtype=out_dtype, device=dev)
+        out = torch.empty((R, N), dtype=out_dtype, device=x.device)
     _expect("x", x, (R, K), dtype, dev)
     _expect("w", w, (N, K), dtype, dev)
     _expect("bias", bias, (N,), out_dtype, dev)
