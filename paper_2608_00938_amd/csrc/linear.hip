@@ -28,7 +28,6 @@ struct E4M3 {
 };
 struct E4M3Wide : E4M3 {};
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-// a chunk at any address: the hardware takes 16-byte loads off their alignment
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
 constexpr int kRowChunks = 8;     // 16-byte chunks of a tile's row: 128 bytes of k
 
@@ -162,103 +161,143 @@ __device__ __forceinline__ void finish4(const LinearArgs& a, int64_t r, int32_t 
   }
 }
 
-// Chunk c of row `row` (clamped into the matrix) at element k, zeros past K.
+// 16 bytes from any element on: the hardware takes them off their alignment.
 template <class T>
-__device__ __forceinline__ u32x4 load_chunk(const void* base, int64_t row, int32_t K, int32_t k) {
+__device__ __forceinline__ u32x4 load16(const typename T::storage* p) { return *(const u32x4_any*)p; }
+
+// 16 bytes of a row of K elements from element k on, zeros past its end.
+template <class T>
+__device__ __forceinline__ u32x4 load_chunk(const typename T::storage* row, int32_t K, int32_t k) {
   constexpr int E = 16 / T::kBytes;
-  const typename T::storage* p = (const typename T::storage*)base + row * K + k;
-  if (k + E <= K) return *(const u32x4_any*)p;
+  if (k + E <= K) return load16<T>(row + k);
+  if (k >= K) return u32x4{0, 0, 0, 0};
+  if (K >= E) {                                            // the row's last 16 bytes, moved down
+    const u32x4 c = load16<T>(row + (K - E));
+    const int bits = (k + E - K) * T::kBytes * 8;          // 8 .. 120
+    const uint64_t lo = (uint64_t)c.y << 32 | c.x, hi = (uint64_t)c.w << 32 | c.z;
+    const uint64_t a = bits >= 64 ? hi >> (bits - 64) : lo >> bits | hi << (64 - bits), b = bits >= 64 ? 0 : hi >> bits;
+    return u32x4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+  }
   u32x4 v = {0, 0, 0, 0};
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     if (k + e < K) {
       uint32_t bits;
-      if constexpr (T::kBytes == 4) bits = __float_as_uint(p[e]);
-      else bits = p[e];
+      if constexpr (T::kBytes == 4) bits = __float_as_uint(row[k + e]);
+      else bits = row[k + e];
       v[e * T::kBytes / 4] |= bits << (e * T::kBytes % 4 * 8);
     }
   }
   return v;
 }
 
-// Four waves, WR x WN of them, of RT x NT tiles of 32 x 32 each; tiles of 128
-// bytes of k pass through registers into LDS, the next one under the products
-// of the current one.  Takes any size and alignment.
-template <class T, int WR, int WN, int RT, int NT>
-__global__ void __launch_bounds__(256) linear_kernel(LinearArgs a) {
-  static_assert(WR * WN == 4, "four waves");
-  constexpr int BR = WR * RT * 32, BN = WN * NT * 32, kPer = (BR + BN) * kRowChunks / 256;
-  constexpr int kTileK = 128 / T::kBytes;
-  using S = Step<T>;
-  __shared__ u32x4 lds[(BR + BN) * kRowChunks];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int half = lane >> 5, col = lane & 31;
-  const int64_t tiles_r = ((int64_t)a.R + BR - 1) / BR;
-  const int64_t r0 = blockIdx.x % tiles_r * BR;
-  const int32_t n0 = (int32_t)(blockIdx.x / tiles_r * BN);
-
-  u32x4 next[kPer];
-  auto fetch = [&](int32_t k0) {
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int chunk = tid + i * 256, row = chunk / kRowChunks;
-      const int32_t k = k0 + chunk % kRowChunks * (16 / T::kBytes);
-      if (row < BR) next[i] = load_chunk<T>(a.x, min(r0 + row, (int64_t)a.R - 1), a.K, k);
-      else next[i] = load_chunk<T>(a.w, min((int64_t)n0 + row - BR, (int64_t)a.N - 1), a.K, k);
-    }
-  };
-  f32x16 acc[RT][NT];
-#pragma unroll
-  for (int i = 0; i < RT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) acc[i][j] = f32x16{0};
-  fetch(0);
-  const int wr = wave / WN * RT * 32, wn = BR + wave % WN * NT * 32;
-  for (int64_t k0 = 0; k0 < a.K; k0 += kTileK) {
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int chunk = tid + i * 256;
-      lds[slot(chunk / kRowChunks, chunk % kRowChunks)] = next[i];
-    }
-    __syncthreads();
-    if (k0 + kTileK < a.K) fetch((int32_t)(k0 + kTileK));
-#pragma unroll
-    for (int s = 0; s < S::kSteps; ++s) {
-      typename S::Frag fr[RT], fn[NT];
-      const auto frag = [&](int row) {
-        u32x4 c[S::kChunks];
-#pragma unroll
-        for (int i = 0; i < S::kChunks; ++i) c[i] = lds[slot(row, (s * 2 + half) * S::kChunks + i)];
-        return S::make(c);
-      };
-#pragma unroll
-      for (int i = 0; i < RT; ++i) fr[i] = frag(wr + i * 32 + col);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) fn[j] = frag(wn + j * 32 + col);
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = S::run(fn[j], fr[i], acc[i][j]);
-    }
+// ---------------------------------------------------------------------------
+// Few rows or few outputs: workgroups of 16 columns x 16 RT rows whose eight waves
+// share out k and add up in LDS.
+//
+// Fragments come from memory in operand layout, without LDS: a lane reads 16 (e4m3:
+// 32) bytes of a row, four lanes 64 or 128 consecutive ones, and several steps are
+// under way at once; what bounds it is reading the weights.  Takes any size and
+// alignment.
+// ---------------------------------------------------------------------------
+template <class T> struct Step16;
+template <> struct Step16<BF16> {
+  static constexpr int kChunks = 1;
+  __device__ __forceinline__ static f32x4 run(const u32x4* a, const u32x4* b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[0]),
+                                                   __builtin_bit_cast(bf16x8, b[0]), c, 0, 0, 0);
   }
-  // (see linear_tile_kernel)
+};
+template <> struct Step16<E4M3> {
+  static constexpr int kChunks = 2;
+  __device__ __forceinline__ static f32x4 run(const u32x4* a, const u32x4* b, f32x4 c) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(Step<E4M3>::make(a), Step<E4M3>::make(b), c, 0, 0,
+                                                            0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+  }
+};
+template <> struct Step16<E4M3Wide> {
+  static constexpr int kChunks = 1;
+  __device__ __forceinline__ static f32x4 run(const u32x4* a, const u32x4* b, f32x4 c) {
+    const auto x = Step<E4M3Wide>::make(a), y = Step<E4M3Wide>::make(b);
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.lo, y.lo, c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.hi, y.hi, c, 0, 0, 0);
+  }
+};
+template <> struct Step16<F32> {
+  static constexpr int kChunks = 1;
+  __device__ __forceinline__ static f32x4 run(const u32x4* a, const u32x4* b, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[0][i]), __uint_as_float(b[0][i]), c, 0, 0, 0);
+    return c;
+  }
+};
+
+constexpr int kFewWaves = 8;
+
+template <class T, int RT>
+__global__ void __launch_bounds__(kFewWaves * 64) linear_few_kernel(LinearArgs a, uint32_t tiles_r) {
+  using S = Step16<T>;
+  constexpr int kStepK = 64 * S::kChunks / T::kBytes;      // of a wave's step
+  constexpr int kUnroll = RT == 1 ? 4 : 2;
+  __shared__ f32x4 sums[kFewWaves][RT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t r0 = (int64_t)(blockIdx.x % tiles_r) * (16 * RT);
+  const int32_t n0 = (int32_t)(blockIdx.x / tiles_r) * 16;
+  const int i16 = lane & 15, part = lane >> 4;
+  const int32_t k_lane = part * (kStepK / 4);
+  const typename T::storage* const w = (const typename T::storage*)a.w + min((int64_t)n0 + i16, (int64_t)a.N - 1) * a.K;
+  const typename T::storage* x[RT];
 #pragma unroll
   for (int i = 0; i < RT; ++i)
+    x[i] = (const typename T::storage*)a.x + min(r0 + i * 16 + i16, (int64_t)a.R - 1) * a.K;
+  constexpr int E = 16 / T::kBytes;
+  f32x4 acc[RT];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(acc[i][j]));
+  for (int i = 0; i < RT; ++i) acc[i] = f32x4{0, 0, 0, 0};
+  // whole steps, kUnroll of them at once, dealt out over the waves
+  const int32_t whole = a.K / kStepK, groups = whole / kUnroll;
+  for (int32_t g = wave; g < groups; g += kFewWaves) {
+    const int32_t k = g * (kUnroll * kStepK) + k_lane;
+    u32x4 fw[kUnroll][S::kChunks], fx[kUnroll][RT][S::kChunks];
 #pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    const int64_t r = r0 + wr + i * 32 + col;
-    if (r >= a.R) continue;
+    for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+      for (int c = 0; c < S::kChunks; ++c) {
+        fw[u][c] = load16<T>(w + k + u * kStepK + c * E);
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float v[4] = {acc[i][j][g * 4], acc[i][j][g * 4 + 1], acc[i][j][g * 4 + 2],
-                            acc[i][j][g * 4 + 3]};
-        finish4(a, r, n0 + (wn - BR) + j * 32 + g * 8 + half * 4, v);
+        for (int i = 0; i < RT; ++i) fx[u][i][c] = load16<T>(x[i] + k + u * kStepK + c * E);
       }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int i = 0; i < RT; ++i) acc[i] = S::run(fw[u], fx[u][i], acc[i]);
+  }
+  // the steps that are left, the last one perhaps short: one a wave (there are at most kUnroll)
+  const int32_t steps = (a.K + kStepK - 1) / kStepK, mine = groups * kUnroll + wave;
+  if (mine < steps) {
+    const int32_t k = mine * kStepK + k_lane;
+    u32x4 fw[S::kChunks], fx[RT][S::kChunks];
+#pragma unroll
+    for (int c = 0; c < S::kChunks; ++c) {
+      fw[c] = load_chunk<T>(w, a.K, k + c * E);
+#pragma unroll
+      for (int i = 0; i < RT; ++i) fx[i][c] = load_chunk<T>(x[i], a.K, k + c * E);
+    }
+#pragma unroll
+    for (int i = 0; i < RT; ++i) acc[i] = S::run(fw, fx[i], acc[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < RT; ++i) sums[wave][i][lane] = acc[i];
+  __syncthreads();
+  // lane l has row l % 16 and columns 4 (l / 16) .. + 3
+  if (wave < RT) {
+    f32x4 y = sums[0][wave][lane];
+#pragma unroll
+    for (int g = 1; g < kFewWaves; ++g) y += sums[g][wave][lane];
+    const int64_t r = r0 + wave * 16 + i16;
+    const float v[4] = {y[0], y[1], y[2], y[3]};
+    if (r < a.R) finish4(a, r, n0 + part * 4, v);
   }
 }
 
@@ -316,7 +355,7 @@ __device__ __forceinline__ void store8(void* p, int64_t i, const float* f) {
 
 // WR x WN waves of RT x NT tiles of 32 x 32: BR rows of x against BN rows of w, in
 // tiles of 128 bytes of k (whole cache lines: with 64 the L2 had twice the requests
-// to serve and was the bound) that alternate between two LDS stages.
+// to serve and was the bound) that go round STAGES places in LDS.
 //
 // Order within a wave.  The products of a step go through the rows of the wave's
 // tile; when a row is done its fragment of the next step is read into the same
@@ -327,10 +366,10 @@ __device__ __forceinline__ void store8(void* p, int64_t i, const float* f) {
 // the stage just left, one or two after each row: all at once they fill the address
 // path's queue and hold up the waves behind them (8192^3 bf16 973 us).
 //
-// Needs 16-byte aligned rows of x and w (k a multiple of a chunk); VEC: outputs
-// whose rows are a multiple of 8 elements and, with bias and residual, 16-byte
+// DIRECT: 16-byte aligned rows of x and w (k a multiple of a chunk), loaded straight
+// into LDS; others pass through registers on the way, a tile behind.  VEC: outputs whose rows are a multiple of 8 elements and, with bias and residual, 16-byte
 // aligned, which leave through LDS as whole lines.
-template <class T, class O, int WR, int WN, int RT, int NT, bool VEC>
+template <class T, class O, int WR, int WN, int RT, int NT, int STAGES, bool VEC, bool DIRECT>
 __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs a, TileMap map) {
   using S = Step<T>;
   constexpr int kTileWaves = WR * WN;
@@ -338,8 +377,10 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
   constexpr int kLoads = kRows / (kTileWaves * 8);         // of 8 rows
   constexpr int kStageBytes = kRows * 128;
   constexpr int kOutBytes = 32 * NT * 128;                 // 32 rows of a wave's sums
-  static_assert(kTileWaves * kOutBytes <= 2 * kStageBytes, "sums fit where the tiles were");
-  __shared__ __attribute__((aligned(256))) char lds[2 * kStageBytes];
+  static_assert(kTileWaves * kOutBytes <= STAGES * kStageBytes, "sums fit where the tiles were");
+  static_assert(DIRECT || STAGES == 2, "registers hold one tile");
+  static_assert((STAGES & (STAGES - 1)) == 0, "tile t lies in stage t % STAGES");
+  __shared__ __attribute__((aligned(256))) char lds[STAGES * kStageBytes];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, col = lane & 31;
 
@@ -368,11 +409,19 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
                    (uint32_t)pitch + chunk * 16;
     }
   }
+  u32x4 held[DIRECT ? 1 : kLoads];
   const auto load = [&](int32_t t, int j) {
+    const char* const from = ((wave + j * kTileWaves) * 8 < BR ? xb : wb) + (int64_t)t * 128;
+    if constexpr (!DIRECT) {
+      constexpr int E = 16 / T::kBytes;
+      if (t < tiles - 1) held[j] = load16<T>((const typename T::storage*)(from + off[j]));
+      else held[j] = load_chunk<T>((const typename T::storage*)(from + (off[j] - chunk * 16)),
+                                   a.K - (tiles - 1) * (128 / T::kBytes), chunk * E);
+      return;
+    }
     // what lies past a row's end reads the row's first chunk of the tile, and is cleared later
     const uint32_t back = t == tiles - 1 && beyond ? chunk * 16 : 0;
-    load_to_lds(((wave + j * kTileWaves) * 8 < BR ? xb : wb) + (int64_t)t * 128, off[j] - back,
-                lds0 + (t & 1) * kStageBytes + (wave + j * kTileWaves) * 1024);
+    load_to_lds(from, off[j] - back, lds0 + (t & (STAGES - 1)) * kStageBytes + (wave + j * kTileWaves) * 1024);
   };
   constexpr int kPerRow = (kLoads + 2 * RT - 1) / (2 * RT); // loads after a row's products
   const auto load_part = [&](int32_t t, int part) {
@@ -381,12 +430,20 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
       if (j < kLoads) load(t, j);
   };
   // Tile t of k has landed, its end is clean, and every wave knows it.
-  const auto hand_over = [&](int32_t t) {
-    wait_loads<0>();
+  const auto hand_over = [&](int32_t t, bool ahead) {
+    if constexpr (!DIRECT) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+        *(u32x4*)(lds + (t & (STAGES - 1)) * kStageBytes + (wave + j * kTileWaves) * 1024 + lane * 16) = held[j];
+      lds_barrier();
+      return;
+    }
+    if (STAGES > 2 && ahead) wait_loads<(STAGES - 2) * kLoads>();   // those of the tiles behind it
+    else wait_loads<0>();
     if (t == tiles - 1 && beyond)
 #pragma unroll
       for (int j = 0; j < kLoads; ++j)
-        *(u32x4*)(lds + (t & 1) * kStageBytes + (wave + j * kTileWaves) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+        *(u32x4*)(lds + (t & (STAGES - 1)) * kStageBytes + (wave + j * kTileWaves) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
     lds_barrier();
   };
 
@@ -403,13 +460,14 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
       c[i] = *(const u32x4*)(row + stage * kStageBytes + (((s * 2 + half) * S::kChunks + i) ^ swz) * 16);
     return S::make(c);
   };
-  // tile t of k; next: there is a tile behind it, more: and one behind that
-  const auto tile = [&](int32_t t, auto next, auto more) {
-    const int stage = t & 1;
+  // tile t of k; next: there is a tile behind it; half: tile t + STAGES - 1 is there, whose
+  // loads are half issued, more: and one behind that
+  const auto tile = [&](int32_t t, auto next, auto half_left, auto more) {
+    const int stage = t & (STAGES - 1), after = (t + 1) & (STAGES - 1);
 #pragma unroll
     for (int s = 0; s < S::kSteps; ++s) {
       const bool last = s + 1 == S::kSteps;
-      const int from = last ? stage ^ 1 : stage, step = last ? 0 : s + 1;
+      const int from = last ? after : stage, step = last ? 0 : s + 1;
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
 #pragma unroll
@@ -417,14 +475,14 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
         __builtin_amdgcn_sched_barrier(0);
         if (!last || next) {
           if (i == 0) {
-            if (last) hand_over(t + 1);
+            if (last) hand_over(t + 1, more);
 #pragma unroll
             for (int j = 0; j < NT; ++j) fn[(s + 1) & 1][j] = frag(wrow + j * 32 * 128, from, step);
           }
           fr[i] = frag(xrow + i * 32 * 128, from, step);
         }
-        if (last && more) load_part(t + 2, i);
-        if (s == 0 && next) load_part(t + 1, RT + i);
+        if (last && more) load_part(t + STAGES, i);
+        if (s == 0 && half_left) load_part(t + STAGES - 1, RT + i);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -433,25 +491,40 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
   struct No { constexpr operator bool() const { return false; } };
 
 #pragma unroll
-  for (int j = 0; j < kLoads; ++j) load(0, j);
-  if (tiles > 1)
-#pragma unroll
-    for (int i = 0; i < RT; ++i) load_part(1, i);
-#pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x16{0};
-  if (tiles > 1) wait_loads<kPerRow * RT < kLoads ? kPerRow * RT : kLoads>();
-  else hand_over(0);
-  if (tiles > 1) lds_barrier();
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) load(0, j);
+#pragma unroll
+  for (int t = 1; t < STAGES - 1; ++t)
+    if (t < tiles)
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) load(t, j);
+  constexpr int kHalf = kPerRow * RT < kLoads ? kPerRow * RT : kLoads;
+  if (DIRECT && tiles >= STAGES) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i) load_part(STAGES - 1, i);
+    wait_loads<(STAGES - 2) * kLoads + kHalf>();
+    lds_barrier();
+  } else {
+    hand_over(0, false);
+    if (!DIRECT && tiles > 1)
+#pragma unroll
+      for (int i = 0; i < RT; ++i) load_part(1, i);
+  }
+  int32_t t = 0;
 #pragma unroll
   for (int j = 0; j < NT; ++j) fn[0][j] = frag(wrow + j * 32 * 128, 0, 0);
 #pragma unroll
   for (int i = 0; i < RT; ++i) fr[i] = frag(xrow + i * 32 * 128, 0, 0);
-  int32_t t = 0;
-  for (; t + 2 < tiles; ++t) tile(t, Yes{}, Yes{});
-  if (t + 1 < tiles) tile(t++, Yes{}, No{});
-  tile(t, No{}, No{});
+  for (; t + STAGES < tiles; ++t) tile(t, Yes{}, Yes{}, Yes{});
+  if constexpr (STAGES == 2) {
+    if (t + 1 < tiles) tile(t++, Yes{}, Yes{}, No{});
+  } else {
+    for (; t + 1 < tiles; ++t) tile(t, Yes{}, t + STAGES - 1 < tiles, No{});
+  }
+  tile(t, No{}, No{}, No{});
   // The products stay out of the epilogue's branches: there the compiler would set the
   // block scales for the lanes that store alone, and the matrix core reads all lanes'.
 #pragma unroll
@@ -526,37 +599,67 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
   }
 }
 
-template <class T, class O, int WR, int WN, int RT, int NT>
+template <class T, class O, int WR, int WN, int RT, int NT, int STAGES>
 hipError_t run_tile(const LinearArgs& a, hipStream_t stream) {
   constexpr int BR = WR * RT * 32, BN = WN * NT * 32, kThreads = WR * WN * 64;
   const uint32_t tiles_r = (uint32_t)(((int64_t)a.R + BR - 1) / BR), tiles_n = (uint32_t)(((int64_t)a.N + BN - 1) / BN);
   const uint32_t all = tiles_r * tiles_n, per = (all + 7) / 8;
   const TileMap map{tiles_r, tiles_n, all, per};
   const uint32_t grid = 8 * per;
+  // rows that start on 16 bytes, of x and w, and of all that the epilogue touches
+  const bool direct = (int64_t)a.K * T::kBytes % 16 == 0 && ((uintptr_t)a.x | (uintptr_t)a.w) % 16 == 0;
   const uintptr_t any = (uintptr_t)a.out | (uintptr_t)a.bias | (uintptr_t)a.residual | (uintptr_t)a.w_scale;
-  if (a.N % 8 == 0 && any % 16 == 0)
-    linear_tile_kernel<T, O, WR, WN, RT, NT, true><<<grid, kThreads, 0, stream>>>(a, map);
-  else
-    linear_tile_kernel<T, O, WR, WN, RT, NT, false><<<grid, kThreads, 0, stream>>>(a, map);
+  const bool vec = a.N % 8 == 0 && any % 16 == 0;
+  const auto go = [&](auto kernel) {
+    kernel<<<grid, kThreads, 0, stream>>>(a, map);
+    return hipGetLastError();
+  };
+  if (direct) {
+    if (vec) return go(linear_tile_kernel<T, O, WR, WN, RT, NT, STAGES, true, true>);
+    return go(linear_tile_kernel<T, O, WR, WN, RT, NT, STAGES, false, true>);
+  }
+  if constexpr (WR * WN == 4) {
+    if (vec) return go(linear_tile_kernel<T, O, WR, WN, RT, NT, 2, true, false>);
+    return go(linear_tile_kernel<T, O, WR, WN, RT, NT, 2, false, false>);
+  }
+  return run_tile<T, O, 2, 2, 2, 2, 2>(a, stream);         // the held tile's registers are not free there
+}
+
+template <class T, int RT>
+hipError_t run_few(const LinearArgs& a, hipStream_t stream) {
+  const uint32_t tiles_r = (uint32_t)(((int64_t)a.R + 16 * RT - 1) / (16 * RT)), tiles_n = ((uint32_t)a.N + 15) / 16;
+  linear_few_kernel<T, RT><<<tiles_r * tiles_n, kFewWaves * 64, 0, stream>>>(a, tiles_r);
   return hipGetLastError();
 }
 
 template <class T, class O>
 hipError_t run(const LinearArgs& a, hipStream_t stream) {
-  // rows that start on 16 bytes, and a tile of them within 32-bit offsets
+  const auto tiles = [&](int br, int bn) {
+    return ((int64_t)a.R + br - 1) / br * (((int64_t)a.N + bn - 1) / bn);
+  };
+  // Few rows: the weights' reading counts, and the few-rows kernel reads them from every
+  // CU (16 x 1024 -> 4096 bf16 4.5 us against 6.4 with 64 x 64 tiles, 32 x 4096 -> 4096
+  // 14.4 against 18.8; 64 x 4096 -> 4096 21.6 against 18.8).  Few tiles of fp32, whose
+  // products take eight times as long, or of rows off 16 bytes too: eight waves share a
+  // tile there (512 x 1024 -> 512 fp32 13 us against 23).
   const int64_t pitch = (int64_t)a.K * T::kBytes;
-  const bool direct = pitch % 16 == 0 && ((uintptr_t)a.x | (uintptr_t)a.w) % 16 == 0 && pitch < (1 << 22);
-  if (direct) {
-    const auto tiles = [&](int br, int bn) {
-      return ((int64_t)a.R + br - 1) / br * (((int64_t)a.N + bn - 1) / bn);
-    };
-    if (tiles(256, 256) >= 256) return run_tile<T, O, 2, 4, 4, 2>(a, stream);
-    if (tiles(128, 128) >= 256) return run_tile<T, O, 2, 2, 2, 2>(a, stream);
-    return run_tile<T, O, 2, 2, 1, 1>(a, stream);
+  const bool slow = T::kBytes == 4 || pitch % 16 != 0;
+  if (a.R <= 32 || (slow && tiles(64, 64) <= 128) || pitch >= (1 << 22)) {
+    if (a.R <= 16) return run_few<T, 1>(a, stream);
+    return a.R <= 32 ? run_few<T, 2>(a, stream) : run_few<T, 4>(a, stream);
   }
-  const int64_t tiles = (((int64_t)a.R + 63) / 64) * (((int64_t)a.N + 63) / 64);
-  linear_kernel<T, 2, 2, 1, 1><<<(uint32_t)tiles, 256, 0, stream>>>(a);
-  return hipGetLastError();
+  // The tile by what it takes in rounds of workgroups over the 256 CUs (one of 256 x 256
+  // or two smaller ones on each) and by its rate: per output 128 x 128 tiles take 1.2
+  // times as long as 256 x 256 and 64 x 64 1.9 times (16384 x 2048 -> 2048 bf16 116, 137
+  // and 215 us); one smaller workgroup on a CU has it to itself.
+  const auto cost = [&](int64_t n, int area, int per_cu, float rate) {
+    const int64_t rounds = n <= 256 ? 1 : (n + 256 * per_cu - 1) / (256 * per_cu) * per_cu;
+    return (float)(rounds * area) * rate;
+  };
+  const float c256 = cost(tiles(256, 256), 256 * 256, 1, 1.f), c128 = cost(tiles(128, 128), 128 * 128, 2, 1.2f),
+              c64 = cost(tiles(64, 64), 64 * 64, 2, 1.9f);
+  if (c64 <= c128 && c64 <= c256) return run_tile<T, O, 2, 2, 1, 1, 4>(a, stream);
+  return c128 <= c256 ? run_tile<T, O, 2, 2, 2, 2, 2>(a, stream) : run_tile<T, O, 2, 4, 4, 2, 2>(a, stream);
 }
 
 template <class T>

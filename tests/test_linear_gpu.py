@@ -210,3 +210,18 @@ def test_more_than_2_31_inputs(gpu):
     torch.cuda.synchronize()
     _check(out[-3:], {k: s[k] for k in ("x", "w", "w_scale")}, "none", F32)
     assert not out[:-3].any()
+
+
+@pytest.mark.parametrize("R,N,K", [(33000, 520, 160), (20000, 1000, 328), (5000, 2056, 250), (70000, 136, 64),
+                                   (33000, 515, 161), (1500, 1500, 1200), (66000, 260, 96), (300, 300, 4104)])
+@pytest.mark.parametrize("dtype,out_dtype", [(F32, F32), (BF16, BF16), (BF16, F32), (E4M3, BF16), (E4M3, F32)])
+def test_many_tiles(gpu, R, N, K, dtype, out_dtype):
+    """Sizes that reach each of the tile sizes, with partial tiles in every direction;
+    the first, last and some other rows."""
+    s = _inputs(gpu, R, N, K, dtype, out_dtype, R + K)
+    want_rows = np.unique(np.r_[0:70, R // 2:R // 2 + 70, R - 300:R])
+    rows = torch.from_numpy(want_rows).to(gpu)
+    got = G.grace_linear(**s, act="silu", out_dtype=out_dtype)
+    torch.cuda.synchronize()
+    _check(got, s, "silu", out_dtype, rows)
+    assert torch.isfinite(got.float()).all()
