@@ -288,9 +288,9 @@ struct RowSampler {
   }
 
   // Narrows the keys [lo, hi), which the border falls into, to one key or one token;
-  // n_before, m_before: candidates and mass above hi.  n_at: candidates left in [lo, hi).
+  // n_before, m_before: candidates and mass above hi.  n_at, m_at: those left in [lo, hi).
   __device__ void narrow(uint32_t& lo, uint32_t& hi, int by, uint32_t n_goal, double m_goal,
-                         uint32_t& n_before, double& m_before, uint32_t& n_at) {
+                         uint32_t& n_before, double& m_before, uint32_t& n_at, double& m_at) {
     while (hi - lo > 1 && n_at > 1) {
       const int shift = max(0, 22 - __builtin_clz(hi - lo - 1));   // (hi - lo - 1) >> shift < 1024
       for (int i = tid; i < kParts; i += NT) s.part_count[i] = 0, s.part_mass[i] = 0;
@@ -302,7 +302,7 @@ struct RowSampler {
           if (x[e] >= least_x && x[e] > -INFINITY && k >= lo && k < hi) {
             const uint32_t i = (hi - 1 - k) >> shift;
             atomicAdd(&s.part_count[i], 1u);
-            if (by) unsafeAtomicAdd(&s.part_mass[i], weight(x[e]));
+            unsafeAtomicAdd(&s.part_mass[i], weight(x[e]));
           }
         }
       });
@@ -315,7 +315,7 @@ struct RowSampler {
         nb = 0, mb = 0;
         for (int j = 0; j < i; ++j) nb += s.part_count[j], mb += s.part_mass[j];
       }
-      n_before += nb, m_before += mb, n_at = s.part_count[i];
+      n_before += nb, m_before += mb, n_at = s.part_count[i], m_at = s.part_mass[i];
       const uint32_t end = hi - ((uint32_t)i << shift), width = 1u << shift;
       lo = end - lo > width ? end - width : lo;
       hi = end;
@@ -393,38 +393,26 @@ struct RowSampler {
         __syncthreads();
       }
       uint32_t lo = 0, hi = 0, n_before, n_at;
-      double m_before, total;
+      double m_before, m_at;
       const auto border = [&](int by, uint32_t n_goal, double m_goal) {
         const int bin = locate(s.count, s.mass, Bins::kCount, by, n_goal, m_goal, n_before, m_before);
         if (bin < 0) return false;
-        n_at = s.count[bin];
+        n_at = s.count[bin], m_at = s.mass[bin];
         bins.keys(bin, lo, hi);
-        if (kMasses || bin == Bins::kSide) narrow(lo, hi, by, n_goal, m_goal, n_before, m_before, n_at);
+        if (kMasses || bin == Bins::kSide) narrow(lo, hi, by, n_goal, m_goal, n_before, m_before, n_at, m_at);
         else lo = order_key(bf16_of_keys(lo, hi));
         return true;
       };
-      total = -1;
+      double total = -1;                                   // the mass that top-k keeps
       if (border(0, rules.k, 0)) {
         cut = key_value(lo);
         ties = rules.k - n_before;
+        total = m_before + (n_at <= ties ? m_at : ties * weight(cut));
         if (n_at <= ties) ties = 0xffffffffu;              // all of them: no rank to keep
       }
       if (rules.p < 1.0) {
-        // the mass that top-k keeps
-        double m = 0;
-        uint32_t n = 0;
-        if (cut > -INFINITY) {
-          sweep(0, a.V, [&](int32_t, const float* x) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              if (x[e] > cut) m += weight(x[e]);
-              n += x[e] == cut;
-            }
-          });
-          m = over_waves(lanes_total(m), s.sums);
-          n = over_waves(lanes_total(n), s.counts);
-          total = m + min(ties, n) * weight(cut);
-        } else {
+        if (total < 0) {
+          double m = 0;
           for (int i = tid; i < Bins::kCount; i += NT) m += s.mass[i];
           total = over_waves(lanes_total(m), s.sums);
         }
@@ -451,10 +439,28 @@ struct RowSampler {
     const double least = rules.least, w_cut = cut > -INFINITY ? weight(cut) : 0.0;
     const bool ranked = ties != 0xffffffffu;
     const double w_tie = w_cut >= least || cut == best ? w_cut : 0.0;
-    const auto kept = [&](float x) {                       // the weight of what is above the cut
+    const auto kept_weight = [&](float x) {                // of what is above the cut
       if (!(ranked ? x > cut : x >= cut) || !(x >= least_x) || !(x > -INFINITY)) return 0.0;
       const double w = weight(x);
       return w >= least || x == best ? w : 0.0;
+    };
+    // of bf16 a table by bins
+    if constexpr (!kMasses) {
+      __syncthreads();
+      for (int i = tid; i < Bins::kCount; i += NT) {
+        uint32_t lo, hi;
+        bins.keys(i, lo, hi);
+        const float x = bf16_of_keys(lo, hi);
+        s.mass[i] = x <= best ? kept_weight(x) : 0.0;
+      }
+      __syncthreads();
+    }
+    const auto kept = [&](float x) {
+      if constexpr (!kMasses) {
+        const int b = bins.of(fmaxf(x, least_x));          // below least_x there is nothing, as at it or below the cut
+        if (b != Bins::kSide) return x >= least_x ? s.mass[b] : 0.0;
+      }
+      return kept_weight(x);
     };
     int32_t lo = 0, hi = a.V;
     double before = 0, goal = -1;
