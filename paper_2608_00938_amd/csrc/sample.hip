@@ -117,41 +117,34 @@ __device__ __forceinline__ double exp2_f64(double x) {
   return ldexp(s, (int)n);
 }
 
-// Bins by value, the largest first: 16 octaves of 128 bins above zero from the one
-// of the row's largest magnitude down, one bin for the smaller values of either
-// sign, 16 octaves below zero.
+// Bins by value, the largest first: kSide bins above zero, 128 to an octave, the last of
+// 16 octaves above the row's largest magnitude; one bin for the smaller values of either
+// sign; kSide below zero.  -inf, +inf and NaN fall into the outermost bins, which no
+// other value of the row does.
 struct Bins {
   static constexpr int kSide = 16 * 128, kCount = 2 * kSide + 1;
-  uint32_t base;                                           // upper half of the least magnitude of a side
+  int base;                                                // upper half of the bits below a side's first bin
   __device__ explicit Bins(float most) {
-    const int e = (int)(__float_as_uint(most) >> 23 & 255) - 15;
-    base = (uint32_t)max(e, 0) << 7;
+    const int e = (int)(__float_as_uint(most) >> 23 & 255) - 14;
+    base = (max(e, 1) << 7) - 1;
   }
-  __device__ int of(float x) const {
-    const uint32_t bits = __float_as_uint(x), high = (bits & 0x7fffffffu) >> 16;
-    if (high < base || high == 0) return kSide;            // 0 itself too, where base is 0
-    const int at = (int)min(high - base, (uint32_t)kSide - 1);
-    return bits >> 31 ? kSide + 1 + at : kSide - 1 - at;
+  __device__ __forceinline__ int of(float x) const {
+    const uint32_t bits = __float_as_uint(x);
+    const int out = min(max((int)(bits >> 16 & 0x7fff) - base, 0), kSide), sign = (int)bits >> 31;
+    return kSide + ((out ^ ~sign) - ~sign);                // + out below zero, - out above
   }
   // Keys of a bin: [lo, hi).
   __device__ void keys(int bin, uint32_t& lo, uint32_t& hi) const {
-    const auto up = [&](int at) {                           // the least key of a bin above zero
-      const uint32_t high = base + (uint32_t)at;
-      return 0x80000000u + (max(high, 1u) << 16);
-    };
-    const auto down = [&](int at) {                         // the key past a bin below zero
-      const uint32_t high = base + (uint32_t)at;
-      return 0x80000000u - (max(high, 1u) << 16);
-    };
+    const int out = bin < kSide ? kSide - bin : bin - kSide;
+    const uint32_t from = (uint32_t)(base + max(out, 1)) << 16, to = from + (1u << 16);   // magnitudes
     if (bin < kSide) {
-      lo = up(kSide - 1 - bin);
-      hi = bin == 0 ? 0xffffffffu : up(kSide - bin);
+      lo = 0x80000000u + from;
+      hi = out == kSide ? 0xffffffffu : 0x80000000u + to;
     } else if (bin == kSide) {
-      lo = down(0), hi = up(0);
+      lo = 0x80000000u - from, hi = 0x80000000u + from;
     } else {
-      const int at = bin - kSide - 1;
-      hi = down(at);
-      lo = at == kSide - 1 ? 0u : down(at + 1);
+      lo = out == kSide ? 0u : 0x80000000u - to;
+      hi = 0x80000000u - from;
     }
   }
 };
@@ -187,42 +180,66 @@ struct RowSampler {
         row((const typename T::storage*)a_.logits + r * a_.V),
         mask(a_.mask ? (const uint8_t*)(a_.mask + r * ((a_.V + 31) / 32)) : nullptr) {}
 
-  // Eight tokens from v on, a multiple of 8: their logits (-inf past the row's end).
-  __device__ void logits(int32_t v, float* x) const {
+  // Eight tokens from v on, a multiple of 8, as they lie in memory (-inf past the row's
+  // end), and their filter bits.
+  struct Raw {
+    u32x4 c[T::kBytes / 2];
+    uint32_t bits;
+  };
+  __device__ __forceinline__ Raw fetch(int32_t v) const {
+    Raw x;
     if (v + 8 <= a.V) {
-      u32x4 c = *(const u32x4_any*)(row + v);
-      Chunk<T>::unpack(c, x);
-      if constexpr (T::kBytes == 4) {
-        c = *(const u32x4_any*)(row + v + 4);
-        Chunk<T>::unpack(c, x + 4);
-      }
-    } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = v + e < a.V ? logit_at<T>(a, r, v + e) : -INFINITY;
+      for (int i = 0; i < T::kBytes / 2; ++i) x.c[i] = *(const u32x4_any*)(row + v + i * 4);
+    } else {
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = v + e < a.V ? logit_at<T>(a, r, v + e) : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < T::kBytes / 2; ++i) x.c[i] = Chunk<T>::pack(f + i * 4);
     }
+    x.bits = mask && v < a.V ? mask[v / 8] : 0xff;
+    return x;
+  }
+  __device__ __forceinline__ static void logits(const Raw& raw, float* x) {
+#pragma unroll
+    for (int i = 0; i < T::kBytes / 2; ++i) Chunk<T>::unpack(raw.c[i], x + i * 4);
   }
   // What is no candidate to -inf: filtered tokens, NaN.
-  __device__ void filter(int32_t v, float* x) const {
-    const uint32_t bits = mask && v < a.V ? mask[v / 8] : 0xff;
+  __device__ __forceinline__ static void filter(const Raw& raw, float* x) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = fmaxf(keep_bit(x[e], bits, e), -INFINITY);
+    for (int e = 0; e < 8; ++e) x[e] = fmaxf(keep_bit(x[e], raw.bits, e), -INFINITY);
   }
-  // f(v, x) for the eights of this wave's piece of [lo, hi) (lo a multiple of 512), -inf
-  // where there is no candidate; pieces are multiples of 512.
+  // f(raw) for the eights of this wave's piece of [lo, hi) (lo a multiple of 512); pieces
+  // are multiples of 512.  The next two eights are under way while f has one: else the
+  // wave waits for the L2 at each.
   __device__ static int32_t piece(int32_t lo, int32_t hi) {
     return ((hi - lo + kWaves - 1) / kWaves + 511) / 512 * 512;
   }
   template <class F>
-  __device__ void sweep(int32_t lo, int32_t hi, F f) const {
+  __device__ __forceinline__ void sweep_raw(int32_t lo, int32_t hi, F f) const {
     const int32_t n = piece(lo, hi), from = lo + wave * n, to = min(hi, from + n);
-    for (int32_t v = from + lane * 8; v - lane * 8 < to; v += 512) {
-      float x[8];
-      logits(v, x);
-      filter(v, x);
-      f(v, x);
+    if (from >= to) return;
+    Raw x = fetch(from + lane * 8), y = x;
+    if (from + 512 < to) y = fetch(from + 512 + lane * 8);
+    for (int32_t v = from; v < to; v += 512) {
+      Raw z = y;
+      if (v + 1024 < to) z = fetch(v + 1024 + lane * 8);
+      f(x);
+      x = y, y = z;
     }
   }
-  __device__ double weight(float x) const {
+  // f(x), the candidates' logits, -inf for others
+  template <class F>
+  __device__ __forceinline__ void sweep(int32_t lo, int32_t hi, F f) const {
+    sweep_raw(lo, hi, [&](const Raw& raw) __attribute__((always_inline)) {
+      float x[8];
+      logits(raw, x);
+      filter(raw, x);
+      f(x);
+    });
+  }
+  __device__ __forceinline__ double weight(float x) const {
     return x == best ? 1.0 : exp2_f64(((double)x - (double)best) * scale);
   }
 
@@ -295,7 +312,7 @@ struct RowSampler {
       const int shift = max(0, 22 - __builtin_clz(hi - lo - 1));   // (hi - lo - 1) >> shift < 1024
       for (int i = tid; i < kParts; i += NT) s.part_count[i] = 0, s.part_mass[i] = 0;
       __syncthreads();
-      sweep(0, a.V, [&](int32_t, const float* x) {
+      sweep(0, a.V, [&](const float* x) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const uint32_t k = order_key(x[e]);
@@ -328,16 +345,15 @@ struct RowSampler {
     // best candidate and largest logit
     float top = -INFINITY, most = -INFINITY;
     {
-      const int32_t n = piece(0, a.V), from = wave * n, to = min(a.V, from + n);
-      for (int32_t v = from + lane * 8; v - lane * 8 < to; v += 512) {
+      sweep_raw(0, a.V, [&](const Raw& raw) __attribute__((always_inline)) {
         float x[8];
-        logits(v, x);
+        logits(raw, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e]);
-        filter(v, x);
+        filter(raw, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) most = fmaxf(most, x[e]);
-      }
+      });
       top = wave_max(top), most = wave_max(most);
       if (lane == 0) s.tops[wave] = top, s.bests[wave] = most;
       for (int i = tid; i < Bins::kCount; i += NT) s.count[i] = 0, s.mass[i] = 0;
@@ -359,24 +375,21 @@ struct RowSampler {
 
     // the row's sum of exp, and the histogram
     float e1 = 0;
-    {
-      const int32_t n = piece(0, a.V), from = wave * n, to = min(a.V, from + n);
-      for (int32_t v = from + lane * 8; v - lane * 8 < to; v += 512) {
-        float x[8];
-        logits(v, x);
+    sweep_raw(0, a.V, [&](const Raw& raw) __attribute__((always_inline)) {
+      float x[8];
+      logits(raw, x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) e1 += fast_exp2((x[e] - top) * kLog2e);   // a NaN or +inf makes it NaN
-        if (!cuts) continue;
-        filter(v, x);
+      for (int e = 0; e < 8; ++e) e1 += fast_exp2((x[e] - top) * kLog2e);   // a NaN or +inf makes it NaN
+      if (!cuts) return;
+      filter(raw, x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (x[e] >= least_x && x[e] > -INFINITY) {
-            const int b = bins.of(x[e]);
-            atomicAdd(&s.count[b], 1u);
-            if (kMasses || b == Bins::kSide) unsafeAtomicAdd(&s.mass[b], weight(x[e]));
-          }
-      }
-    }
+      for (int e = 0; e < 8; ++e)
+        if (x[e] >= least_x && x[e] > -INFINITY) {
+          const int b = bins.of(x[e]);
+          atomicAdd(&s.count[b], 1u);
+          if (kMasses || b == Bins::kSide) unsafeAtomicAdd(&s.mass[b], weight(x[e]));
+        }
+    });
     const float log_sum = logf((float)over_waves((double)wave_sum(e1), s.sums));
 
     // kept: values above cut, and the first `ties` tokens of value cut
@@ -439,7 +452,7 @@ struct RowSampler {
     const double least = rules.least, w_cut = cut > -INFINITY ? weight(cut) : 0.0;
     const bool ranked = ties != 0xffffffffu;
     const double w_tie = w_cut >= least || cut == best ? w_cut : 0.0;
-    const auto kept_weight = [&](float x) {                // of what is above the cut
+    const auto kept_weight = [&](float x) __attribute__((always_inline)) {                // of what is above the cut
       if (!(ranked ? x > cut : x >= cut) || !(x >= least_x) || !(x > -INFINITY)) return 0.0;
       const double w = weight(x);
       return w >= least || x == best ? w : 0.0;
@@ -451,16 +464,36 @@ struct RowSampler {
         uint32_t lo, hi;
         bins.keys(i, lo, hi);
         const float x = bf16_of_keys(lo, hi);
-        s.mass[i] = x <= best ? kept_weight(x) : 0.0;
+        s.mass[i] = x <= best && i != Bins::kSide ? kept_weight(x) : 0.0;
       }
       __syncthreads();
     }
-    const auto kept = [&](float x) {
+    const auto kept = [&](float x) __attribute__((always_inline)) {
       if constexpr (!kMasses) {
-        const int b = bins.of(fmaxf(x, least_x));          // below least_x there is nothing, as at it or below the cut
-        if (b != Bins::kSide) return x >= least_x ? s.mass[b] : 0.0;
+        const int b = bins.of(x);
+        if (b != Bins::kSide) return s.mass[b];
       }
       return kept_weight(x);
+    };
+    // of eight tokens; those next to zero are few, and asked for once
+    const auto kept_sum = [&](const float* x) __attribute__((always_inline)) {
+      double m = 0;
+      if constexpr (kMasses) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m += kept_weight(x[e]);
+      } else {
+        bool some = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int b = bins.of(x[e]);
+          some |= b == Bins::kSide;
+          m += s.mass[b];                                  // of that bin 0
+        }
+        if (some)
+          for (int e = 0; e < 8; ++e)
+            if (bins.of(x[e]) == Bins::kSide) m += kept_weight(x[e]);
+      }
+      return m;
     };
     int32_t lo = 0, hi = a.V;
     double before = 0, goal = -1;
@@ -468,12 +501,11 @@ struct RowSampler {
     while (hi - lo > 512 || goal < 0) {
       double m = 0;
       uint32_t n = 0;
-      sweep(lo, hi, [&](int32_t, const float* x) {
+      sweep(lo, hi, [&](const float* x) __attribute__((always_inline)) {
+        m += kept_sum(x);
+        if (ranked)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          m += kept(x[e]);
-          n += ranked && x[e] == cut;
-        }
+          for (int e = 0; e < 8; ++e) n += x[e] == cut;
       });
       m = lanes_total(m), n = lanes_total(n);
       __syncthreads();
@@ -511,8 +543,11 @@ struct RowSampler {
     if (wave > 0) return;
     float x[8];
     const int32_t v0 = lo + lane * 8;
-    logits(v0, x);
-    filter(v0, x);
+    {
+      const Raw raw = fetch(v0);
+      logits(raw, x);
+      filter(raw, x);
+    }
     uint32_t n = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) n += ranked && x[e] == cut;
@@ -919,7 +954,7 @@ __device__ __forceinline__ int32_t sample_wave(const float (&x)[N], float best, 
 }
 
 template <class T, int NCH>
-__global__ void __launch_bounds__(256) sample_wave_kernel(SampleArgs a) {
+__global__ void __launch_bounds__(256, NCH == 8 ? 1 : 2) sample_wave_kernel(SampleArgs a) {
   constexpr int N = NCH * 8;
   __shared__ WaveBins bins[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -992,6 +1027,7 @@ hipError_t run(const SampleArgs& a, hipStream_t stream) {
   if (a.V <= 512) sample_wave_kernel<T, 1><<<waves, 256, 0, stream>>>(a);
   else if (a.V <= 1024) sample_wave_kernel<T, 2><<<waves, 256, 0, stream>>>(a);
   else if (a.V <= 2048) sample_wave_kernel<T, 4><<<waves, 256, 0, stream>>>(a);
+  else if (a.V <= 4096) sample_wave_kernel<T, 8><<<waves, 256, 0, stream>>>(a);
   else if (a.V <= 8192) sample_row_kernel<T, 256><<<a.R, 256, 0, stream>>>(a);
   else sample_row_kernel<T, 1024><<<a.R, 1024, 0, stream>>>(a);
   return hipGetLastError();
