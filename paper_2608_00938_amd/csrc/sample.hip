@@ -63,6 +63,39 @@ __device__ __forceinline__ float uniform(float x) {
 }
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float shifted(float x) {
+  return __builtin_bit_cast(
+      float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, ROWS, 0xF, false));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double shifted(double x) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xF, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xF, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// Sum over the lanes up to this one, in the vector ALU.
+template <class F>
+__device__ __forceinline__ F wave_upto(F x) {
+  x += shifted<0x111, 0xF>(x);   // row_shr:1
+  x += shifted<0x112, 0xF>(x);   // row_shr:2
+  x += shifted<0x114, 0xF>(x);   // row_shr:4
+  x += shifted<0x118, 0xF>(x);   // row_shr:8
+  x += shifted<0x142, 0xA>(x);   // row_bcast:15
+  x += shifted<0x143, 0xC>(x);   // row_bcast:31
+  return x;
+}
+__device__ __forceinline__ float lane_of(float x, int l) { return lane_value(x, l); }
+__device__ __forceinline__ double lane_of(double x, int l) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, l);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), l);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_total(double x) { return lane_of(wave_upto(x), 63); }
+__device__ __forceinline__ float wave_total(float x) { return uniform(wave_sum(x)); }
+
 // A request's rules, as every row of it applies them.
 struct Rules {
   double T;            // 0: the best candidate; finite
@@ -253,18 +286,13 @@ struct RowSampler {
     for (int w = 0; w < kWaves; ++w) all += scratch[w];
     return all;
   }
+  __device__ __forceinline__ static double lanes_upto(double x) { return wave_upto(x); }
+  __device__ __forceinline__ static uint32_t lanes_upto(uint32_t x) { return wave_scan(x); }
   template <class V>
-  __device__ static V lanes_total(V x) {
-    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
-    return x;
-  }
-  template <class V>
-  __device__ static V lanes_upto(V x) {
-    for (int d = 1; d < 64; d <<= 1) {
-      const V y = __shfl_up(x, d);
-      if ((int)(threadIdx.x & 63) >= d) x += y;
-    }
-    return x;
+  __device__ __forceinline__ static V lanes_total(V x) {
+    const V upto = lanes_upto(x);
+    if constexpr (sizeof(V) == 8) return lane_of(upto, 63);
+    else return (V)__builtin_amdgcn_readlane((int)upto, 63);
   }
 
   // In a histogram of n bins: the first bin with which the count reaches n_goal (by =
@@ -316,7 +344,7 @@ struct RowSampler {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const uint32_t k = order_key(x[e]);
-          if (x[e] >= least_x && x[e] > -INFINITY && k >= lo && k < hi) {
+          if (x[e] >= least_x && k >= lo && k < hi) {
             const uint32_t i = (hi - 1 - k) >> shift;
             atomicAdd(&s.part_count[i], 1u);
             unsafeAtomicAdd(&s.part_mass[i], weight(x[e]));
@@ -369,8 +397,9 @@ struct RowSampler {
     const bool greedy = !(rules.T > 0);
     const double temp = greedy ? 1.0 : rules.T;
     scale = 1.4426950408889634 / temp;
-    least_x = greedy ? best : (float)((double)best - (u < 0x1p-30f ? 1100 : 63) * 0.6931471805599453 * temp);
-    const Bins bins(fmaxf(fabsf(best), least_x > -FLT_MAX ? fabsf(least_x) : FLT_MAX));
+    // (finite, so that it keeps -inf out too)
+    least_x = greedy ? best : fmaxf((float)((double)best - (u < 0x1p-30f ? 1100 : 63) * 0.6931471805599453 * temp), -FLT_MAX);
+    const Bins bins(fmaxf(fabsf(best), fabsf(least_x)));
     const bool cuts = !greedy && (rules.k < (uint32_t)a.V || rules.p < 1.0);
 
     // the row's sum of exp, and the histogram
@@ -384,7 +413,7 @@ struct RowSampler {
       filter(raw, x);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (x[e] >= least_x && x[e] > -INFINITY) {
+        if (x[e] >= least_x) {
           const int b = bins.of(x[e]);
           atomicAdd(&s.count[b], 1u);
           if (kMasses || b == Bins::kSide) unsafeAtomicAdd(&s.mass[b], weight(x[e]));
@@ -417,7 +446,7 @@ struct RowSampler {
         return true;
       };
       double total = -1;                                   // the mass that top-k keeps
-      if (border(0, rules.k, 0)) {
+      if (rules.k < (uint32_t)a.V && border(0, rules.k, 0)) {
         cut = key_value(lo);
         ties = rules.k - n_before;
         total = m_before + (n_at <= ties ? m_at : ties * weight(cut));
@@ -453,7 +482,7 @@ struct RowSampler {
     const bool ranked = ties != 0xffffffffu;
     const double w_tie = w_cut >= least || cut == best ? w_cut : 0.0;
     const auto kept_weight = [&](float x) __attribute__((always_inline)) {                // of what is above the cut
-      if (!(ranked ? x > cut : x >= cut) || !(x >= least_x) || !(x > -INFINITY)) return 0.0;
+      if (!(ranked ? x > cut : x >= cut) || !(x >= least_x)) return 0.0;
       const double w = weight(x);
       return w >= least || x == best ? w : 0.0;
     };
@@ -476,6 +505,7 @@ struct RowSampler {
       return kept_weight(x);
     };
     // of eight tokens; those next to zero are few, and asked for once
+    const float from = fmaxf(cut, least_x);
     const auto kept_sum = [&](const float* x) __attribute__((always_inline)) {
       double m = 0;
       if constexpr (kMasses) {
@@ -485,6 +515,7 @@ struct RowSampler {
         bool some = false;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
+          if (!(x[e] >= from)) continue;                   // most: LDS has fewer lanes to serve
           const int b = bins.of(x[e]);
           some |= b == Bins::kSide;
           m += s.mass[b];                                  // of that bin 0
@@ -606,37 +637,6 @@ __global__ void __launch_bounds__(NT) sample_row_kernel(SampleArgs a) {
 // Masses are fp32 as long as they lie further from every border than they can be
 // off; a row for which that fails (one in a thousand) is decided by fp64 masses.
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ double wave_total(double x) {
-  for (int s = 32; s > 0; s >>= 1) x += __shfl_xor(x, s);
-  return x;
-}
-__device__ __forceinline__ float wave_total(float x) { return uniform(wave_sum(x)); }
-// Sum over the lanes up to this one.
-__device__ __forceinline__ double wave_upto(double x) {
-  const int lane = threadIdx.x & 63;
-  for (int d = 1; d < 64; d <<= 1) {
-    const double y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ float shifted(float x) {
-  return __builtin_bit_cast(
-      float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, ROWS, 0xF, false));
-}
-__device__ __forceinline__ float wave_upto(float x) {
-  x += shifted<0x111, 0xF>(x);   // row_shr:1
-  x += shifted<0x112, 0xF>(x);   // row_shr:2
-  x += shifted<0x114, 0xF>(x);   // row_shr:4
-  x += shifted<0x118, 0xF>(x);   // row_shr:8
-  x += shifted<0x142, 0xA>(x);   // row_bcast:15
-  x += shifted<0x143, 0xC>(x);   // row_bcast:31
-  return x;
-}
-__device__ __forceinline__ double lane_of(double x, int l) { return __shfl(x, l); }
-__device__ __forceinline__ float lane_of(float x, int l) { return lane_value(x, l); }
-
 constexpr uint32_t kAll = 0xffffffffu;
 constexpr int kWaveBins = 256;
 struct WaveBins {
