@@ -225,3 +225,42 @@ def test_many_tiles(gpu, R, N, K, dtype, out_dtype):
     torch.cuda.synchronize()
     _check(got, s, "silu", out_dtype, rows)
     assert torch.isfinite(got.float()).all()
+
+
+@pytest.mark.parametrize("R,N,K", [(130, 200, 64), (300, 264, 104), (200, 4000, 100), (20, 30, 40)])
+@pytest.mark.parametrize("x_size,w_size", [(2.0 ** -100, 1.0), (2.0 ** -118, 2.0 ** 20), (2.0 ** 100, 2.0 ** -60),
+                                           (2.0 ** -60, 2.0 ** 60), (2.0 ** 120, 2.0 ** -100)])
+def test_fp32_of_any_size(gpu, R, N, K, x_size, w_size):
+    """Products next to either end of fp32's range are as exact as others."""
+    s = _inputs(gpu, R, N, K, F32, F32, 31, bias=False, residual=False)
+    s = {"x": s["x"] * x_size, "w": s["w"] * w_size}
+    got = G.grace_linear(**s)
+    torch.cuda.synchronize()
+    _check(got, s, "none", F32)
+
+
+@pytest.mark.parametrize("R,N,K", [(200, 300, 64), (300, 264, 33), (20, 30, 40)])
+def test_fp32_infinities_and_largest_values(gpu, R, N, K):
+    """As sums of products: an infinity times a number of either sign is one, times 0 NaN;
+    the largest fp32 stays finite."""
+    s = _inputs(gpu, R, N, K, F32, F32, 37, bias=True, residual=True)
+    s["w"][3] = 0.0
+    s["x"][5, 2] = float("inf")
+    s["x"][9, K - 1] = torch.finfo(F32).max
+    s["w"][:, K - 1] *= 2.0 ** -20
+    s["w"][7, 0] = float("-inf")
+    got = G.grace_linear(**s).cpu().numpy()
+    torch.cuda.synchronize()
+    with np.errstate(invalid="ignore"):
+        want = (s["x"].cpu().double() @ s["w"].cpu().double().t() + s["bias"].cpu().double() +
+                s["residual"].cpu().double()).numpy()
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.isnan(want[5, 3])
+    inf = np.isinf(want)
+    assert np.array_equal(got[inf], want[inf].astype(np.float32)) and inf[5].sum() > N // 2
+    fine = np.isfinite(want)
+    assert np.isfinite(got[fine]).all()
+    # the tolerance of the other tests, where neither row nor column holds an infinity
+    with np.errstate(invalid="ignore"):
+        A = np.abs(s["x"].cpu().double().numpy()) @ np.abs(s["w"].cpu().double().numpy()).T
+        tol = 1.13 * (K + 28) * STEP * (A + 8)
+    assert (np.abs(got[fine] - want[fine]) <= tol[fine]).all()
