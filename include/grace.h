@@ -438,10 +438,6 @@ int32_t grace_trie_advance(const grace_gtm_index* index, const int32_t* node_pre
                            int32_t M_prev, int32_t k, int32_t* node_next, int32_t* err_flag,
                            void* stream);
 
-/* Bytes of device workspace grace_sample needs for B, M, V (-1 if out of range;
- * may be 0). */
-int64_t grace_sample_workspace_bytes(int32_t B, int32_t M, int32_t V);
-
 /*
  * Sampled continuation of every beam row, where grace_beam_step searches: row r =
  * b*M + m draws one token from its logits under request b's rules.  (The rows then
@@ -478,21 +474,16 @@ int64_t grace_sample_workspace_bytes(int32_t B, int32_t M, int32_t V);
  *   B, M, V      requests, rows per request, vocabulary; B, M >= 0 (B*M = 0 is a
  *                no-op), 1 <= V <= 2^24, B*M below 2^31, B*M*V below 2^40
  *   dtype        GRACE_F32 or GRACE_BF16 (of the logits)
- *   workspace    device, at least grace_sample_workspace_bytes(B, M, V) bytes,
- *                8-byte aligned, caller-owned; contents on entry are ignored and on
- *                return unspecified; calls that share it must not overlap (NULL
- *                where none is needed)
  *   tokens       device, int32 [B*M]
  *   scores       device, fp32 [B*M]; may be prev_scores itself
  *   stream       hipStream_t
- * Apart from scores in place, outputs and the workspace must not overlap each
- * other or the inputs.
+ * Apart from scores in place, the outputs must not overlap each other or the
+ * inputs.
  */
 int32_t grace_sample(const void* logits, const float* uniform, const float* prev_scores,
                      const uint32_t* mask, const float* temperature, const int32_t* top_k,
                      const float* top_p, const float* min_p, int32_t B, int32_t M, int32_t V,
-                     int32_t dtype, void* workspace, int64_t workspace_bytes, int32_t* tokens,
-                     float* scores, void* stream);
+                     int32_t dtype, int32_t* tokens, float* scores, void* stream);
 
 /* Longest row grace_rms_norm accepts (32768). */
 int32_t grace_rms_norm_max_d(void);

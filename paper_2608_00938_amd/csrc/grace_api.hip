@@ -560,23 +560,15 @@ bool good_sample_sizes(int32_t B, int32_t M, int32_t V) {
 
 extern "C" {
 
-int64_t grace_sample_workspace_bytes(int32_t B, int32_t M, int32_t V) {
-  return good_sample_sizes(B, M, V) ? grace::sample_workspace_bytes(B, M, V) : -1;
-}
-
 int32_t grace_sample(const void* logits, const float* uniform, const float* prev_scores,
                      const uint32_t* mask, const float* temperature, const int32_t* top_k,
                      const float* top_p, const float* min_p, int32_t B, int32_t M, int32_t V,
-                     int32_t dtype, void* workspace, int64_t workspace_bytes, int32_t* tokens,
-                     float* scores, void* stream) {
+                     int32_t dtype, int32_t* tokens, float* scores, void* stream) {
   if (dtype != GRACE_F32 && dtype != GRACE_BF16) return GRACE_ERR_UNSUPPORTED;
   if (!good_sample_sizes(B, M, V)) return GRACE_ERR_SHAPE;
   const int64_t R = (int64_t)B * M;
   if (R == 0) return GRACE_OK;
   if (!logits || !uniform || !tokens || !scores) return GRACE_ERR_NULL;
-  const int64_t need = grace::sample_workspace_bytes(B, M, V);
-  if (need > 0 && !workspace) return GRACE_ERR_NULL;
-  if (workspace_bytes < need || (need > 0 && ((uintptr_t)workspace & 7) != 0)) return GRACE_ERR_SHAPE;
   const Range reads[8] = {{logits, R * V * elem_bytes(dtype)},
                           {uniform, R * 4},
                           {mask, mask ? R * ((V + 31) / 32) * 4 : 0},
@@ -585,10 +577,9 @@ int32_t grace_sample(const void* logits, const float* uniform, const float* prev
                           {top_p, top_p ? (int64_t)B * 4 : 0},
                           {min_p, min_p ? (int64_t)B * 4 : 0},
                           {prev_scores, prev_scores ? R * 4 : 0}};
-  const Range writes[3] = {{tokens, R * 4}, {scores, R * 4}, {workspace, need}};
-  for (int i = 0; i < 3; ++i) {
-    for (int j = i + 1; j < 3; ++j)
-      if (overlaps(writes[i].p, writes[i].n, writes[j].p, writes[j].n)) return GRACE_ERR_ALIAS;
+  const Range writes[2] = {{tokens, R * 4}, {scores, R * 4}};
+  if (overlaps(tokens, R * 4, scores, R * 4)) return GRACE_ERR_ALIAS;
+  for (int i = 0; i < 2; ++i) {
     for (int j = 0; j < 8; ++j) {
       // the rows' scores may be updated in place
       if (i == 1 && j == 7 && scores == prev_scores) continue;
@@ -596,8 +587,8 @@ int32_t grace_sample(const void* logits, const float* uniform, const float* prev
     }
   }
   return hip_status(grace::launch_sample(logits, uniform, prev_scores, mask, temperature, top_k,
-                                         top_p, min_p, B, M, V, dtype == GRACE_BF16, workspace,
-                                         tokens, scores, (hipStream_t)stream));
+                                         top_p, min_p, B, M, V, dtype == GRACE_BF16, tokens, scores,
+                                         (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -84,14 +84,11 @@ hipError_t launch_linear(const void* x, const float* x_scale, const void* w, con
                          hipStream_t stream);
 
 // A token of every row by temperature, top-k, top-p and min-p (each per request, or
-// null), and prev (or 0) + its log-probability; workspace of
-// sample_workspace_bytes(B, M, V) bytes.
+// null), and prev (or 0) + its log-probability.
 hipError_t launch_sample(const void* logits, const float* uniform, const float* prev,
                          const uint32_t* mask, const float* temperature, const int32_t* top_k,
                          const float* top_p, const float* min_p, int32_t B, int32_t M, int32_t V,
-                         bool bf16, void* workspace, int32_t* tokens, float* scores,
-                         hipStream_t stream);
-int64_t sample_workspace_bytes(int32_t B, int32_t M, int32_t V);
+                         bool bf16, int32_t* tokens, float* scores, hipStream_t stream);
 
 // Debug builds: add the device-check counters of the attention kernels' source
 // files to acc[0 .. 7] and clear them (synchronous); release builds return

@@ -1035,12 +1035,10 @@ hipError_t run(const SampleArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-int64_t sample_workspace_bytes(int32_t, int32_t, int32_t) { return 0; }
-
 hipError_t launch_sample(const void* logits, const float* uniform, const float* prev,
                          const uint32_t* mask, const float* temperature, const int32_t* top_k,
                          const float* top_p, const float* min_p, int32_t B, int32_t M, int32_t V,
-                         bool bf16, void*, int32_t* tokens, float* scores, hipStream_t stream) {
+                         bool bf16, int32_t* tokens, float* scores, hipStream_t stream) {
   const SampleArgs a{logits, uniform, prev, mask, temperature, top_k, top_p, min_p, tokens, scores,
                      B * M, M, V};
   return bf16 ? run<BF16>(a, stream) : run<F32>(a, stream);

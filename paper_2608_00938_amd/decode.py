@@ -132,8 +132,6 @@ class DecodeLoop:
                 raise ValueError("sampled rows keep their places: all widths must be equal")
             own = torch.arange(Mmax, dtype=torch.int32, device=dev).repeat(B, 1)
             self.parents = [own] * self.T
-            ws = max(G.grace_sample_workspace_bytes(B, Mmax, V), 8)
-            self.workspace = torch.empty((ws,), dtype=torch.uint8, device=dev)
         self.gtm = gtm
         if gtm is not None:
             W = (V + 31) // 32
@@ -165,8 +163,7 @@ class DecodeLoop:
             if self.sampling is not None:
                 G.grace_sample(self.logits[t], self.sampling.uniform[t], B, M, mask=self.masks[t],
                                prev_scores=prev, tokens=self.tokens[t].view(-1),
-                               scores=self.scores[t].view(-1), workspace=self.workspace,
-                               **self.sampling.rules)
+                               scores=self.scores[t].view(-1), **self.sampling.rules)
             else:
                 # score update + top-k in one call: no [B*M, V] candidate array
                 G.grace_beam_step(self.logits[t], prev, B, M, self.k_out[t], mask=self.masks[t],

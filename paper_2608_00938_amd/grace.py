@@ -76,10 +76,8 @@ _SIGNATURES = {
                        _c_int, _c_void_p, _c_void_p, _c_void_p],
     "grace_trie_advance": [ctypes.POINTER(GtmIndexC), _c_void_p, _c_void_p, _c_void_p, _c_int,
                            _c_int, _c_int, _c_void_p, _c_void_p, _c_void_p],
-    "grace_sample_workspace_bytes": [_c_int, _c_int, _c_int],
     "grace_sample": [_c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p,
-                     _c_void_p, _c_int, _c_int, _c_int, _c_int, _c_void_p, ctypes.c_int64, _c_void_p,
-                     _c_void_p, _c_void_p],
+                     _c_void_p, _c_int, _c_int, _c_int, _c_int, _c_void_p, _c_void_p, _c_void_p],
     "grace_rms_norm_max_d": [],
     "grace_rms_norm": [_c_void_p, _c_void_p, _c_void_p, _c_int, _c_int, _c_float, _c_int, _c_int,
                        _c_void_p, _c_void_p, _c_void_p, _c_void_p],
@@ -474,20 +472,14 @@ def _call(fn: str, like: torch.Tensor, *args):
         raise GraceError(st, fn)
 
 
-def grace_sample_workspace_bytes(B: int, M: int, V: int) -> int:
-    return library().grace_sample_workspace_bytes(B, M, V)
-
-
 def grace_sample(logits, uniform, B: int, M: int, temperature=None, top_k=None, top_p=None,
-                 min_p=None, mask=None, prev_scores=None, tokens=None, scores=None, workspace=None):
+                 min_p=None, mask=None, prev_scores=None, tokens=None, scores=None):
     """One token for each of the B*M rows of logits [B*M, V] (fp32 or bf16), drawn with
     uniform fp32 [B*M] under its request's temperature, top_p, min_p (fp32 [B]) and
     top_k (int32 [B]), each a device tensor or None; mask and prev_scores as for
     grace_beam_scores.  Returns (tokens int32 [B*M], scores fp32 [B*M]): the scores are
     prev_scores plus the tokens' log-probabilities; a row without candidates gets
-    token -1 and score -inf.  ``scores`` may be prev_scores itself.  ``workspace``: a
-    device uint8 tensor of at least grace_sample_workspace_bytes(B, M, V) bytes
-    (allocated here when not given and needed)."""
+    token -1 and score -inf.  ``scores`` may be prev_scores itself."""
     R, V = logits.shape
     dev, f32, i32 = logits.get_device(), torch.float32, torch.int32
     code = _dtype_code(logits)
@@ -507,18 +499,9 @@ def grace_sample(logits, uniform, B: int, M: int, temperature=None, top_k=None, 
         scores = torch.empty((R,), dtype=f32, device=logits.device)
     _expect("tokens", tokens, (R,), i32, dev)
     _expect("scores", scores, (R,), f32, dev)
-    size = 0
-    if workspace is None:
-        need = grace_sample_workspace_bytes(B, M, V)
-        if need > 0:
-            workspace = torch.empty((need,), dtype=torch.uint8, device=logits.device)
-            size = need
-    else:
-        _expect("workspace", workspace, workspace.shape, workspace.dtype, dev)
-        size = workspace.numel() * workspace.element_size()
     _call("grace_sample", logits, _ptr(logits), _ptr(uniform), _ptr(prev_scores), _ptr(mask),
-          _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), B, M, V, code, _ptr(workspace),
-          size, _ptr(tokens), _ptr(scores))
+          _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), B, M, V, code, _ptr(tokens),
+          _ptr(scores))
     return tokens, scores
 
 

@@ -156,11 +156,10 @@ def test_oracle_linear_by_hand():
 
 def sample(**kw):
     a = dict(z=at(1), u=at(2), prev=at(3), mask=at(4), T=at(5), k=at(6), p=at(7), m=at(8), B=2, M=4, V=64,
-             dtype=G.GRACE_BF16, ws=at(9), size=1 << 20, tok=at(10), sc=at(11))
+             dtype=G.GRACE_BF16, tok=at(10), sc=at(11))
     a.update(kw)
     return G.library().grace_sample(a["z"], a["u"], a["prev"], a["mask"], a["T"], a["k"], a["p"], a["m"],
-                                    a["B"], a["M"], a["V"], a["dtype"], a["ws"], a["size"], a["tok"], a["sc"],
-                                    None)
+                                    a["B"], a["M"], a["V"], a["dtype"], a["tok"], a["sc"], None)
 
 
 @needs_lib
@@ -180,24 +179,6 @@ def sample(**kw):
 ])
 def test_sample_rejects(kw, status):
     assert sample(**kw) == status
-
-
-@needs_lib
-def test_sample_workspace():
-    lib = G.library()
-    assert lib.grace_sample_workspace_bytes(-1, 1, 8) == -1
-    assert lib.grace_sample_workspace_bytes(1, 1, 0) == -1
-    assert lib.grace_sample_workspace_bytes(1 << 16, 1 << 15, 8) == -1
-    for B, M, V in ((0, 1, 8), (1, 1, 1 << 24), (64, 4096, 512), (1, 1, 128000)):
-        need = lib.grace_sample_workspace_bytes(B, M, V)
-        assert 0 <= need < 1 << 30
-        if need > 0:
-            kw = dict(B=B, M=M, V=V, u=at(64), prev=at(96), mask=at(128), T=at(192), k=at(193), p=at(194),
-                      m=at(195), tok=at(200), sc=at(216), ws=at(256))
-            assert sample(**kw, size=need - 1) == G.GRACE_ERR_SHAPE
-            assert sample(**{**kw, "ws": None}, size=need) == G.GRACE_ERR_NULL
-            assert sample(**{**kw, "ws": ctypes.c_void_p((256 << 24) + 4)}, size=need) == G.GRACE_ERR_SHAPE
-            assert sample(**{**kw, "ws": at(1)}, size=need) == G.GRACE_ERR_ALIAS
 
 
 def test_sample_binding_checks_every_tensor(monkeypatch):

@@ -232,11 +232,10 @@ def test_other_stream_and_graph_replays(gpu, B, M, V):
     k = torch.full((B,), 60, dtype=torch.int32, device=gpu)
     want, ws = G.grace_sample(logits, u, B, M, temperature=T, top_k=k, top_p=p)
     tokens, scores = torch.empty_like(want), torch.empty_like(ws)
-    work = torch.empty((max(8, G.grace_sample_workspace_bytes(B, M, V)),), dtype=torch.uint8, device=gpu)
     stream = torch.cuda.Stream()
     torch.cuda.synchronize()
     call = lambda: G.grace_sample(logits, u, B, M, temperature=T, top_k=k, top_p=p, tokens=tokens,  # noqa: E731
-                                  scores=scores, workspace=work)
+                                  scores=scores)
     with torch.cuda.stream(stream):
         call()
     stream.synchronize()
@@ -245,8 +244,7 @@ def test_other_stream_and_graph_replays(gpu, B, M, V):
     for rep in range(3):
         tokens.fill_(-5)
         scores.fill_(7)
-        work.fill_(rep + 1)
-        G.grace_sample(logits, u, B, M, workspace=work)      # eager work between the replays
+        G.grace_sample(logits, u, B, M)            # eager work between the replays
         torch.cuda.synchronize()
         graph.launch(stream)
         stream.synchronize()
