@@ -9,6 +9,19 @@
 
 namespace grace {
 
+// launch(first, count) for workgroups first .. first + count - 1 until all are under
+// way: one launch takes fewer than 2^32 threads, 2^22 of the largest workgroups.
+template <class F>
+hipError_t launch_in_parts(int64_t workgroups, F launch) {
+  constexpr int64_t kMost = (int64_t)1 << 21;
+  for (int64_t first = 0; first < workgroups; first += kMost) {
+    launch((uint32_t)first, (uint32_t)(workgroups - first < kMost ? workgroups - first : kMost));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 // Cross-attention, beam-as-query: grid over (request, head, beam tile).
 hipError_t launch_cross_attn(const void* q, const void* enc_k, const void* enc_v,
                              const int32_t* enc_off, void* out, int32_t B, int32_t M, int32_t H,

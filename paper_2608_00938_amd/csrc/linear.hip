@@ -236,14 +236,15 @@ template <> struct Step16<F32> {
 constexpr int kFewWaves = 8;
 
 template <class T, int RT>
-__global__ void __launch_bounds__(kFewWaves * 64) linear_few_kernel(LinearArgs a, uint32_t tiles_r) {
+__global__ void __launch_bounds__(kFewWaves * 64) linear_few_kernel(LinearArgs a, uint32_t tiles_r, uint32_t first) {
   using S = Step16<T>;
   constexpr int kStepK = 64 * S::kChunks / T::kBytes;      // of a wave's step
   constexpr int kUnroll = RT == 1 ? 4 : 2;
   __shared__ f32x4 sums[kFewWaves][RT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t r0 = (int64_t)(blockIdx.x % tiles_r) * (16 * RT);
-  const int32_t n0 = (int32_t)(blockIdx.x / tiles_r) * 16;
+  const uint32_t id = first + blockIdx.x;
+  const int64_t r0 = (int64_t)(id % tiles_r) * (16 * RT);
+  const int32_t n0 = (int32_t)(id / tiles_r) * 16;
   const int i16 = lane & 15, part = lane >> 4;
   const int32_t k_lane = part * (kStepK / 4);
   const typename T::storage* const w = (const typename T::storage*)a.w + min((int64_t)n0 + i16, (int64_t)a.N - 1) * a.K;
@@ -370,7 +371,7 @@ __device__ __forceinline__ void store8(void* p, int64_t i, const float* f) {
 // into LDS; others pass through registers on the way, a tile behind.  VEC: outputs whose rows are a multiple of 8 elements and, with bias and residual, 16-byte
 // aligned, which leave through LDS as whole lines.
 template <class T, class O, int WR, int WN, int RT, int NT, int STAGES, bool VEC, bool DIRECT>
-__global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs a, TileMap map) {
+__global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs a, TileMap map, uint32_t first) {
   using S = Step<T>;
   constexpr int kTileWaves = WR * WN;
   constexpr int BR = WR * RT * 32, BN = WN * NT * 32, kRows = BR + BN;
@@ -394,7 +395,7 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
   const bool beyond = chunk >= last_chunks;                // in the last tile: past k's end
   const uint32_t lds0 = lds_addr(lds);
   uint32_t tr, tn;
-  if (!map.take(blockIdx.x, tr, tn)) return;
+  if (!map.take(first + blockIdx.x, tr, tn)) return;
   const int64_t r0 = (int64_t)tr * BR;
   const int32_t n0 = (int32_t)(tn * BN);
   const char* const xb = (const char*)a.x + r0 * pitch;
@@ -611,8 +612,9 @@ hipError_t run_tile(const LinearArgs& a, hipStream_t stream) {
   const uintptr_t any = (uintptr_t)a.out | (uintptr_t)a.bias | (uintptr_t)a.residual | (uintptr_t)a.w_scale;
   const bool vec = a.N % 8 == 0 && any % 16 == 0;
   const auto go = [&](auto kernel) {
-    kernel<<<grid, kThreads, 0, stream>>>(a, map);
-    return hipGetLastError();
+    return launch_in_parts(grid, [&](uint32_t first, uint32_t count) {
+      kernel<<<count, kThreads, 0, stream>>>(a, map, first);
+    });
   };
   if (direct) {
     if (vec) return go(linear_tile_kernel<T, O, WR, WN, RT, NT, STAGES, true, true>);
@@ -628,8 +630,9 @@ hipError_t run_tile(const LinearArgs& a, hipStream_t stream) {
 template <class T, int RT>
 hipError_t run_few(const LinearArgs& a, hipStream_t stream) {
   const uint32_t tiles_r = (uint32_t)(((int64_t)a.R + 16 * RT - 1) / (16 * RT)), tiles_n = ((uint32_t)a.N + 15) / 16;
-  linear_few_kernel<T, RT><<<tiles_r * tiles_n, kFewWaves * 64, 0, stream>>>(a, tiles_r);
-  return hipGetLastError();
+  return launch_in_parts((int64_t)tiles_r * tiles_n, [&](uint32_t first, uint32_t count) {
+    linear_few_kernel<T, RT><<<count, kFewWaves * 64, 0, stream>>>(a, tiles_r, first);
+  });
 }
 
 template <class T, class O>

@@ -108,11 +108,11 @@ template <class T, int NT, int NG, int OUT>
 __global__ void __launch_bounds__(NT == 64 ? 256 : NT)
 rms_norm_kernel(const typename T::storage* x, const typename T::storage* residual,
                 const typename T::storage* weight, typename T::storage* sum, void* out,
-                float* out_scale, int32_t R, int32_t D, float eps) {
+                float* out_scale, int32_t R, int32_t D, float eps, uint32_t first) {
   __shared__ float scratch[2][NT / 64];
   constexpr int kRows = NT == 64 ? 4 : 1;      // rows of a workgroup
   const int lane = threadIdx.x % NT;
-  const int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / NT;
+  const int64_t r = (int64_t)(first + blockIdx.x) * kRows + threadIdx.x / NT;
   if (r >= R) return;                          // whole waves of a one-wave row only
   constexpr int E = Chunk<T>::kElems;
   constexpr int kOutBytes = OUT == GRACE_F32 ? 4 : (OUT == GRACE_BF16 ? 2 : 1);
@@ -194,10 +194,11 @@ template <class T, int NT, int NG, int OUT>
 hipError_t run(const NormArgs& a) {
   using S = typename T::storage;
   const int64_t rows = NT == 64 ? 4 : 1;
-  rms_norm_kernel<T, NT, NG, OUT><<<(uint32_t)((a.R + rows - 1) / rows), NT == 64 ? 256 : NT, 0, a.stream>>>(
-      (const S*)a.x, (const S*)a.residual, (const S*)a.weight, (S*)a.sum, a.out, a.scale, a.R, a.D,
-      a.eps);
-  return hipGetLastError();
+  return launch_in_parts((a.R + rows - 1) / rows, [&](uint32_t first, uint32_t count) {
+    rms_norm_kernel<T, NT, NG, OUT><<<count, NT == 64 ? 256 : NT, 0, a.stream>>>(
+        (const S*)a.x, (const S*)a.residual, (const S*)a.weight, (S*)a.sum, a.out, a.scale, a.R, a.D,
+        a.eps, first);
+  });
 }
 
 // Groups per lane, the least power of two that holds the row.

@@ -38,6 +38,7 @@ struct SampleArgs {
   int32_t *tokens;
   float* scores;
   int32_t R, M, V;
+  uint32_t first;              // of the launch's workgroups
 };
 
 constexpr float kMostUniform = 1.f - 0x1p-24f;   // the largest fp32 below 1
@@ -208,7 +209,7 @@ struct RowSampler {
   float least_x;                                           // candidates from here on count
 
   __device__ RowSampler(const SampleArgs& a_, Shared& s_)
-      : a(a_), s(s_), r(blockIdx.x), tid(threadIdx.x), lane(tid & 63),
+      : a(a_), s(s_), r(a_.first + blockIdx.x), tid(threadIdx.x), lane(tid & 63),
         wave(__builtin_amdgcn_readfirstlane(tid >> 6)),
         row((const typename T::storage*)a_.logits + r * a_.V),
         mask(a_.mask ? (const uint8_t*)(a_.mask + r * ((a_.V + 31) / 32)) : nullptr) {}
@@ -958,7 +959,7 @@ __global__ void __launch_bounds__(256, NCH == 8 ? 1 : 2) sample_wave_kernel(Samp
   constexpr int N = NCH * 8;
   __shared__ WaveBins bins[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t r = (int64_t)blockIdx.x * 4 + wave;
+  const int64_t r = (int64_t)(a.first + blockIdx.x) * 4 + wave;
   if (r >= a.R) return;                                    // whole waves
   const Rules rules(a, (int32_t)(r / a.M));
   float x[N];
@@ -1022,15 +1023,17 @@ __global__ void __launch_bounds__(256, NCH == 8 ? 1 : 2) sample_wave_kernel(Samp
 }
 
 template <class T>
-hipError_t run(const SampleArgs& a, hipStream_t stream) {
-  const uint32_t waves = (uint32_t)(((int64_t)a.R + 3) / 4);
-  if (a.V <= 512) sample_wave_kernel<T, 1><<<waves, 256, 0, stream>>>(a);
-  else if (a.V <= 1024) sample_wave_kernel<T, 2><<<waves, 256, 0, stream>>>(a);
-  else if (a.V <= 2048) sample_wave_kernel<T, 4><<<waves, 256, 0, stream>>>(a);
-  else if (a.V <= 4096) sample_wave_kernel<T, 8><<<waves, 256, 0, stream>>>(a);
-  else if (a.V <= 8192) sample_row_kernel<T, 256><<<a.R, 256, 0, stream>>>(a);
-  else sample_row_kernel<T, 1024><<<a.R, 1024, 0, stream>>>(a);
-  return hipGetLastError();
+hipError_t run(SampleArgs a, hipStream_t stream) {
+  const int64_t workgroups = a.V <= 4096 ? ((int64_t)a.R + 3) / 4 : a.R;
+  return launch_in_parts(workgroups, [&](uint32_t first, uint32_t count) {
+    a.first = first;
+    if (a.V <= 512) sample_wave_kernel<T, 1><<<count, 256, 0, stream>>>(a);
+    else if (a.V <= 1024) sample_wave_kernel<T, 2><<<count, 256, 0, stream>>>(a);
+    else if (a.V <= 2048) sample_wave_kernel<T, 4><<<count, 256, 0, stream>>>(a);
+    else if (a.V <= 4096) sample_wave_kernel<T, 8><<<count, 256, 0, stream>>>(a);
+    else if (a.V <= 8192) sample_row_kernel<T, 256><<<count, 256, 0, stream>>>(a);
+    else sample_row_kernel<T, 1024><<<count, 1024, 0, stream>>>(a);
+  });
 }
 
 }  // namespace
@@ -1040,7 +1043,7 @@ hipError_t launch_sample(const void* logits, const float* uniform, const float* 
                          const float* top_p, const float* min_p, int32_t B, int32_t M, int32_t V,
                          bool bf16, int32_t* tokens, float* scores, hipStream_t stream) {
   const SampleArgs a{logits, uniform, prev, mask, temperature, top_k, top_p, min_p, tokens, scores,
-                     B * M, M, V};
+                     B * M, M, V, 0};
   return bf16 ? run<BF16>(a, stream) : run<F32>(a, stream);
 }
 
