@@ -1,5 +1,6 @@
 """The position-wise entry points at ends of their ranges: more workgroups than one
-launch takes."""
+launch takes, the tails of the activations, scales whose product leaves fp32."""
+import math
 import sys
 
 import numpy as np
@@ -10,7 +11,7 @@ from paper_2608_00938_amd import grace as G
 
 pytestmark = pytest.mark.gpu
 
-BF16 = torch.bfloat16
+F32, BF16 = torch.float32, torch.bfloat16
 
 
 def _log(msg):
@@ -65,3 +66,40 @@ def test_sample_of_very_many_rows(gpu, R, V):
         assert torch.equal(tokens[c], first.to(torch.int32)), c
         want = -(x[c].float() - top.float()).exp().sum(1).log()
         assert ((scores[c] - want).abs() <= 2.0 ** -16 * (1 + want.abs())).all(), c
+
+
+def _tails():
+    """y as bf16, where gelu(y) is a normal number."""
+    y = torch.cat([torch.linspace(-12, 12, 3000), -torch.logspace(-30, 1, 600), torch.logspace(-30, 1, 600)])
+    return y.to(BF16)
+
+
+@pytest.mark.parametrize("out_dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [16, 2048])
+def test_gelu_keeps_relative_accuracy_in_its_tails(gpu, rows, out_dtype):
+    """y (1 + erf) / 2 = y erfc(-y / sqrt 2) / 2.  The exponent y^2 / 2 (in powers of two at
+    most 72 nepers here) is off by 5.5 * 2^-24 of itself: the rounded factor 1 / sqrt 2 (half) and
+    product, both squared, log2(e) (half) and two products.  That is 2.4e-5 of the value; the
+    rest, the tail's approximation among it, is below 2^-19 (32 steps).  Together less than
+    2^-15, and the output's rounding."""
+    y = _tails()
+    x = torch.zeros(rows, 8, dtype=BF16)
+    w = torch.zeros(8, 8, dtype=BF16)
+    w[:, 0] = 1
+    for i in range(0, len(y), rows):
+        part = y[i:i + rows]
+        x[:len(part), 0] = part
+        got = G.grace_linear(x.to(gpu), w.to(gpu), act="gelu", out_dtype=out_dtype)[:len(part)].double().cpu()
+        want = torch.tensor([v * math.erfc(-v / math.sqrt(2)) / 2 for v in part.tolist()], dtype=torch.float64)
+        tol = want.abs() * (2.0 ** -15 + torch.finfo(out_dtype).eps / 2)
+        assert ((got - want[:, None]).abs() <= tol[:, None]).all()
+
+
+@pytest.mark.parametrize("R,N", [(3, 8), (100, 8), (100, 7)])
+def test_scales_whose_product_leaves_fp32(gpu, R, N):
+    """Powers of two, so that every order without an underflow is exact."""
+    x = torch.full((R, 8), 2.0 ** 60, dtype=BF16, device=gpu)
+    w = torch.full((N, 8), 2.0 ** 57, dtype=BF16, device=gpu)
+    xs, ws = torch.full((R,), 2.0 ** -100, device=gpu), torch.full((N,), 2.0 ** -60, device=gpu)
+    out = G.grace_linear(x, w, x_scale=xs, w_scale=ws, out_dtype=F32)
+    assert (out == 2.0 ** -40).all()
