@@ -457,7 +457,8 @@ int32_t grace_trie_advance(const grace_gtm_index* index, const int32_t* node_pre
  *                whole vocabulary at temperature 1, as grace_beam_scores; NaN where
  *                the row has a NaN or +inf logit.
  * A row without candidates gets token -1 and score -inf; grace_trie_advance takes
- * it to node -1, a dead beam.  Every choice is the one that fp64 arithmetic makes.
+ * it to node -1, a dead beam.  Every choice is the one that fp64 arithmetic makes,
+ * in rows above 4096 tokens up to 2^-39 of the row's mass.
  *
  *   logits       device, [B*M, V], dtype
  *   uniform      device, fp32 [B*M]; random numbers in [0, 1) (others are clamped

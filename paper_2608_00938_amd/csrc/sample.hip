@@ -123,12 +123,15 @@ struct Rules {
 // next to zero, are cut again by their keys where a border falls into them.  A
 // sweep then adds up the kept weights of each wave's piece of the vocabulary, the
 // piece with the drawn token is dealt out again over the waves, and so on down to
-// 512 tokens, which one wave goes through.
+// 512 tokens, which one wave goes through.  32 rows of 128000 bf16 take 74 us, bound by
+// the vector ALU of the 32 CUs and the chain of steps; up to 8192 tokens 256 threads
+// have the shorter chain, and two rows share a CU.
 //
 // All sums are fp64, whose exp2 costs a sweep some 90 cycles per wave of tokens; of
-// bf16 only the bins need it.  Candidates whose weight is below 2^-63 are left out:
-// all of a row's together are below 2^-39 of the total, a part that decides nothing
-// but draws with u below 2^-30, which leave none out.
+// bf16 only the bins need it.  fp32 bins are added by fp64 atomics in no fixed order,
+// which moves a mass by less than 2^-40 of the row's.  Candidates whose weight is below
+// 2^-63 are left out: all of a row's together are below 2^-39 of the total, a part that
+// decides nothing but draws with u below 2^-30, which leave none out.
 // ---------------------------------------------------------------------------
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
 

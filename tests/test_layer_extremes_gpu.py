@@ -3,7 +3,6 @@ launch takes, the tails of the activations, scales whose product leaves fp32."""
 import math
 import sys
 
-import numpy as np
 import pytest
 import torch
 
