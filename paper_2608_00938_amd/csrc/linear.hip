@@ -344,18 +344,34 @@ struct TileMap {
   }
 };
 
-// Eight values at element i, a multiple of 8, of a 16-byte aligned tensor.
-template <class O>
-__device__ __forceinline__ void load8(const void* p, int64_t i, float* f) {
-  const u32x4* v = (const u32x4*)((const char*)p + i * O::kBytes);
-  Chunk<O>::unpack(v[0], f);
-  if constexpr (O::kBytes == 4) Chunk<O>::unpack(v[1], f + 4);
+// Eight values from element i on, at any alignment, or the first `left` of them (EIGHTS:
+// none or eight).
+template <class O, bool EIGHTS>
+__device__ __forceinline__ void load8(const void* p, int64_t i, int left, float* f) {
+  const typename O::storage* at = (const typename O::storage*)p + i;
+  if (EIGHTS ? left > 0 : left >= 8) {
+#pragma unroll
+    for (int c = 0; c < O::kBytes / 2; ++c) Chunk<O>::unpack(load16<O>(at + c * 4), f + c * 4);
+  } else if (!EIGHTS) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) f[e] = load_out_type(at, e, O::kBytes == 4 ? GRACE_F32 : GRACE_BF16);
+  }
 }
-template <class O>
-__device__ __forceinline__ void store8(void* p, int64_t i, const float* f) {
-  u32x4* v = (u32x4*)((char*)p + i * O::kBytes);
-  v[0] = Chunk<O>::pack(f);
-  if constexpr (O::kBytes == 4) v[1] = Chunk<O>::pack(f + 4);
+template <class O, bool EIGHTS>
+__device__ __forceinline__ void store8(void* p, int64_t i, int left, const float* f) {
+  typename O::storage* at = (typename O::storage*)p + i;
+  if (EIGHTS ? left > 0 : left >= 8) {
+#pragma unroll
+    for (int c = 0; c < O::kBytes / 2; ++c) *(u32x4_any*)(at + c * 4) = Chunk<O>::pack(f + c * 4);
+  } else if (!EIGHTS) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) {
+        if constexpr (O::kBytes == 4) at[e] = f[e];
+        else at[e] = (uint16_t)pack_bf16x2(f[e], 0.f);
+      }
+  }
 }
 
 // WR x WN waves of RT x NT tiles of 32 x 32: BR rows of x against BN rows of w, in
@@ -372,16 +388,17 @@ __device__ __forceinline__ void store8(void* p, int64_t i, const float* f) {
 // path's queue and hold up the waves behind them (8192^3 bf16 973 us).
 //
 // DIRECT: 16-byte aligned rows of x and w (k a multiple of a chunk), loaded straight
-// into LDS; others pass through registers on the way, a tile behind.  VEC: outputs
-// whose rows are a multiple of 8 elements and which, with bias, residual and w_scale,
-// are 16-byte aligned; they leave through LDS as whole lines.
+// into LDS; others pass through registers on the way.  EIGHTS: N is a multiple of 8,
+// which saves a branch at each store (262144 x 1024 -> 4096 e4m3 1500 -> 1475 us).
+// Other outputs leave as whole lines as well, at any alignment: stored one by one from
+// the accumulators 262144 x 512 -> 509 bf16 took 748 us instead of 188.
 //
 // What bounds it: of a long k the matrix core (8192^3 bf16 829 us = 1326 TFLOP/s, 76 %
 // busy; e4m3 426 us = 2580), of a short one what is not under products.  Of 262144 x
 // 1024 -> 4096 e4m3 with silu (1464 us, 495 of them writes at the copy rate) a 256 x 256
 // tile spends some 5 thousand cycles on its first loads, 3 thousand on each of 8 tiles
 // of k (2 thousand of products) and 10 to 15 thousand on its epilogue.
-template <class T, class O, int WR, int WN, int RT, int NT, int STAGES, bool VEC, bool DIRECT>
+template <class T, class O, int WR, int WN, int RT, int NT, int STAGES, bool EIGHTS, bool DIRECT>
 __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs a, TileMap map, uint32_t first) {
   using S = Step<T>;
   constexpr int kTileWaves = WR * WN;
@@ -390,7 +407,11 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
   constexpr int kStageBytes = kRows * 128;
   constexpr int kOutBytes = 32 * NT * 128;                 // 32 rows of a wave's sums
   static_assert(kTileWaves * kOutBytes <= STAGES * kStageBytes, "sums fit where the tiles were");
-  static_assert(DIRECT || STAGES == 2, "registers hold one tile");
+  // Tiles of k under way in registers: three where they are small (2000 x 1021 -> 509 bf16
+  // 12.5 us with one, 10.8 with three; of e4m3, 2000 x 1001 -> 1000, 11.2 and 12.1).
+  constexpr int kHeld = !DIRECT && RT * NT == 1 && T::kBytes > 1 ? 3 : 1;
+  constexpr int kAhead = DIRECT ? STAGES : kHeld + 1;      // tile t + kAhead is loaded when t + 1 is handed over
+  static_assert(DIRECT || STAGES == 2, "a tile read, a tile written");
   static_assert((STAGES & (STAGES - 1)) == 0, "tile t lies in stage t % STAGES");
   __shared__ __attribute__((aligned(256))) char lds[STAGES * kStageBytes];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -421,13 +442,13 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
                    (uint32_t)pitch + chunk * 16;
     }
   }
-  u32x4 held[DIRECT ? 1 : kLoads];
-  const auto load = [&](int32_t t, int j) {
+  u32x4 held[kHeld][DIRECT ? 1 : kLoads];
+  const auto load = [&](int32_t t, int h, int j) __attribute__((always_inline)) {
     const char* const from = ((wave + j * kTileWaves) * 8 < BR ? xb : wb) + (int64_t)t * 128;
     if constexpr (!DIRECT) {
       constexpr int E = 16 / T::kBytes;
-      if (t < tiles - 1) held[j] = load16<T>((const typename T::storage*)(from + off[j]));
-      else held[j] = load_chunk<T>((const typename T::storage*)(from + (off[j] - chunk * 16)),
+      if (t < tiles - 1) held[h][j] = load16<T>((const typename T::storage*)(from + off[j]));
+      else held[h][j] = load_chunk<T>((const typename T::storage*)(from + (off[j] - chunk * 16)),
                                    a.K - (tiles - 1) * (128 / T::kBytes), chunk * E);
       return;
     }
@@ -436,17 +457,17 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
     load_to_lds(from, off[j] - back, lds0 + (t & (STAGES - 1)) * kStageBytes + (wave + j * kTileWaves) * 1024);
   };
   constexpr int kPerRow = (kLoads + 2 * RT - 1) / (2 * RT); // loads after a row's products
-  const auto load_part = [&](int32_t t, int part) {
+  const auto load_part = [&](int32_t t, int h, int part) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = part * kPerRow; j < (part + 1) * kPerRow; ++j)
-      if (j < kLoads) load(t, j);
+      if (j < kLoads) load(t, h, j);
   };
   // Tile t of k has landed, its end is clean, and every wave knows it.
-  const auto hand_over = [&](int32_t t, bool ahead) {
+  const auto hand_over = [&](int32_t t, int h, bool ahead) __attribute__((always_inline)) {
     if constexpr (!DIRECT) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j)
-        *(u32x4*)(lds + (t & (STAGES - 1)) * kStageBytes + (wave + j * kTileWaves) * 1024 + lane * 16) = held[j];
+        *(u32x4*)(lds + (t & (STAGES - 1)) * kStageBytes + (wave + j * kTileWaves) * 1024 + lane * 16) = held[h][j];
       lds_barrier();
       return;
     }
@@ -464,7 +485,7 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
   const int swz = col >> 1 & 7;
   const char* const xrow = lds + (wr + col) * 128;
   const char* const wrow = lds + (BR + wn + col) * 128;
-  typename S::Frag fr[RT], fn[2][NT];
+  typename S::Frag fr[RT == 1 ? 2 : RT], fn[2][NT];
   const auto frag = [&](const char* row, int stage, int s) {
     u32x4 c[S::kChunks];
 #pragma unroll
@@ -472,14 +493,31 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
       c[i] = *(const u32x4*)(row + stage * kStageBytes + (((s * 2 + half) * S::kChunks + i) ^ swz) * 16);
     return S::make(c);
   };
-  // tile t of k; next: there is a tile behind it; half: tile t + STAGES - 1 is there, whose
-  // loads are half issued, more: and one behind that
-  const auto tile = [&](int32_t t, auto next, auto half_left, auto more) {
+  // tile t of k, whose registers are h of held; next: there is a tile behind it; half: tile
+  // t + kAhead - 1 is there, whose loads are half issued, more: and one behind that
+  const auto tile = [&](int32_t t, int h, auto next, auto half_left, auto more) __attribute__((always_inline)) {
     const int stage = t & (STAGES - 1), after = (t + 1) & (STAGES - 1);
 #pragma unroll
     for (int s = 0; s < S::kSteps; ++s) {
       const bool last = s + 1 == S::kSteps;
       const int from = last ? after : stage, step = last ? 0 : s + 1;
+      // no other row's products to read under: fragments a step ahead (2000 x 1021 -> 509 fp32
+      // 32.8 -> 31.2 us; e4m3, two steps a tile, was slower)
+      if constexpr (RT == 1 && S::kSteps == 4) {
+        if (!last || next) {
+          if (last) hand_over(t + 1, (h + 1) % kHeld, more);
+#pragma unroll
+          for (int j = 0; j < NT; ++j) fn[(s + 1) & 1][j] = frag(wrow + j * 32 * 128, from, step);
+          fr[(s + 1) & 1] = frag(xrow, from, step);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[0][j] = S::run(fn[s & 1][j], fr[s & 1], acc[0][j]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (last && more) load_part(t + kAhead, (h + 1) % kHeld, 0);
+        if (s == 0 && half_left) load_part(t + kAhead - 1, h, 1);
+        continue;
+      }
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
 #pragma unroll
@@ -487,14 +525,14 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
         __builtin_amdgcn_sched_barrier(0);
         if (!last || next) {
           if (i == 0) {
-            if (last) hand_over(t + 1, more);
+            if (last) hand_over(t + 1, (h + 1) % kHeld, more);
 #pragma unroll
             for (int j = 0; j < NT; ++j) fn[(s + 1) & 1][j] = frag(wrow + j * 32 * 128, from, step);
           }
           fr[i] = frag(xrow + i * 32 * 128, from, step);
         }
-        if (last && more) load_part(t + STAGES, i);
-        if (s == 0 && half_left) load_part(t + STAGES - 1, RT + i);
+        if (last && more) load_part(t + kAhead, (h + 1) % kHeld, i);
+        if (s == 0 && half_left) load_part(t + kAhead - 1, h, RT + i);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -507,36 +545,46 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x16{0};
 #pragma unroll
-  for (int j = 0; j < kLoads; ++j) load(0, j);
+  for (int j = 0; j < kLoads; ++j) load(0, 0, j);
 #pragma unroll
-  for (int t = 1; t < STAGES - 1; ++t)
+  for (int t = 1; t < kAhead - 1; ++t)
     if (t < tiles)
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) load(t, j);
+      for (int j = 0; j < kLoads; ++j) load(t, t % kHeld, j);
   constexpr int kHalf = kPerRow * RT < kLoads ? kPerRow * RT : kLoads;
   if (DIRECT && tiles >= STAGES) {
 #pragma unroll
-    for (int i = 0; i < RT; ++i) load_part(STAGES - 1, i);
+    for (int i = 0; i < RT; ++i) load_part(STAGES - 1, 0, i);
     wait_loads<(STAGES - 2) * kLoads + kHalf>();
     lds_barrier();
   } else {
-    hand_over(0, false);
-    if (!DIRECT && tiles > 1)
+    hand_over(0, 0, false);
+    if (!DIRECT && tiles > kAhead - 1)
 #pragma unroll
-      for (int i = 0; i < RT; ++i) load_part(1, i);
+      for (int i = 0; i < RT; ++i) load_part(kAhead - 1, 0, i);
   }
   int32_t t = 0;
 #pragma unroll
   for (int j = 0; j < NT; ++j) fn[0][j] = frag(wrow + j * 32 * 128, 0, 0);
 #pragma unroll
   for (int i = 0; i < RT; ++i) fr[i] = frag(xrow + i * 32 * 128, 0, 0);
-  for (; t + STAGES < tiles; ++t) tile(t, Yes{}, Yes{}, Yes{});
-  if constexpr (STAGES == 2) {
-    if (t + 1 < tiles) tile(t++, Yes{}, Yes{}, No{});
+  if constexpr (kHeld > 1) {
+    for (; t + kHeld - 1 + kAhead < tiles; t += kHeld)
+#pragma unroll
+      for (int h = 0; h < kHeld; ++h) tile(t + h, h, Yes{}, Yes{}, Yes{});
+    for (; t < tiles; t += kHeld)
+#pragma unroll
+      for (int h = 0; h < kHeld; ++h)
+        if (t + h < tiles) tile(t + h, h, t + h + 1 < tiles, t + h + kAhead - 1 < tiles, t + h + kAhead < tiles);
   } else {
-    for (; t + 1 < tiles; ++t) tile(t, Yes{}, t + STAGES - 1 < tiles, No{});
+    for (; t + STAGES < tiles; ++t) tile(t, 0, Yes{}, Yes{}, Yes{});
+    if constexpr (STAGES == 2) {
+      if (t + 1 < tiles) tile(t++, 0, Yes{}, Yes{}, No{});
+    } else {
+      for (; t + 1 < tiles; ++t) tile(t, 0, Yes{}, t + STAGES - 1 < tiles, No{});
+    }
+    tile(t, 0, No{}, No{}, No{});
   }
-  tile(t, No{}, No{}, No{});
   // The products stay out of the epilogue's branches: there the compiler would set the
   // block scales for the lanes that store alone, and the matrix core reads all lanes'.
 #pragma unroll
@@ -548,65 +596,49 @@ __global__ void __launch_bounds__(WR * WN * 64, 2) linear_tile_kernel(LinearArgs
   // Epilogue.  In the accumulators lane l has row l % 32 and, of every 8 columns, 4 (l /
   // 32) .. + 3; 32 rows at a time they go through LDS of the wave's own, so that a
   // lane has 8 columns, the same for all its rows, and rows leave as whole lines.
-  if constexpr (VEC) {
-    constexpr int kRowChunk = NT * 8, kLanes = kRowChunk / 2, kPer = 32 * kLanes / 64;
-    const auto at = [&](int row, int c) {                   // 16 rows of one chunk on different banks
-      const int turn = kRowChunk == 16 ? row : row >> 1;
-      return row * NT * 128 + (c ^ (turn & (kRowChunk - 1))) * 16;
-    };
-    char* const mine = lds + wave * kOutBytes;
-    const int row_in = lane / kLanes, c = lane % kLanes * 2;
-    const int32_t n = n0 + wn + c * 4;
-    const bool in = n < a.N;
-    float ws[8], bias[8], xs[RT][kPer];
+  constexpr int kRowChunk = NT * 8, kLanes = kRowChunk / 2, kPer = 32 * kLanes / 64;
+  const auto at = [&](int row, int c) {                   // 16 rows of one chunk on different banks
+    const int turn = kRowChunk == 16 ? row : row >> 1;
+    return row * NT * 128 + (c ^ (turn & (kRowChunk - 1))) * 16;
+  };
+  char* const mine = lds + wave * kOutBytes;
+  const int row_in = lane / kLanes, c = lane % kLanes * 2;
+  const int32_t n = n0 + wn + c * 4;
+  const int left = EIGHTS ? (n < a.N ? 8 : 0) : a.N - n;  // of the lane's columns
+  float ws[8], bias[8], xs[RT][kPer];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ws[e] = 1.f, bias[e] = 0.f;
-    if (a.w_scale && in) load8<F32>(a.w_scale, n, ws);
-    if (a.bias && in) load8<O>(a.bias, n, bias);
+  for (int e = 0; e < 8; ++e) ws[e] = 1.f, bias[e] = 0.f;
+  if (a.w_scale) load8<F32, EIGHTS>(a.w_scale, n, left, ws);
+  if (a.bias) load8<O, EIGHTS>(a.bias, n, left, bias);
 #pragma unroll
-    for (int i = 0; i < RT; ++i)
+  for (int i = 0; i < RT; ++i)
 #pragma unroll
-      for (int q = 0; q < kPer; ++q)
-        xs[i][q] = a.x_scale ? a.x_scale[min(r0 + wr + i * 32 + q * (64 / kLanes) + row_in, (int64_t)a.R - 1)] : 1.f;
+    for (int q = 0; q < kPer; ++q)
+      xs[i][q] = a.x_scale ? a.x_scale[min(r0 + wr + i * 32 + q * (64 / kLanes) + row_in, (int64_t)a.R - 1)] : 1.f;
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
+  for (int i = 0; i < RT; ++i) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *(f32x4*)(mine + at(col, j * 8 + g * 2 + half)) =
-              f32x4{acc[i][j][g * 4], acc[i][j][g * 4 + 1], acc[i][j][g * 4 + 2], acc[i][j][g * 4 + 3]};
+      for (int g = 0; g < 4; ++g)
+        *(f32x4*)(mine + at(col, j * 8 + g * 2 + half)) =
+            f32x4{acc[i][j][g * 4], acc[i][j][g * 4 + 1], acc[i][j][g * 4 + 2], acc[i][j][g * 4 + 3]};
 #pragma unroll
-      for (int q = 0; q < kPer; ++q) {
-        const int row = q * (64 / kLanes) + row_in;
-        const int64_t r = r0 + wr + i * 32 + row;
-        float y[8], res[8];
-        *(f32x4*)y = *(const f32x4*)(mine + at(row, c));
-        *(f32x4*)(y + 4) = *(const f32x4*)(mine + at(row, c + 1));
-        if (r >= a.R || !in) continue;
-        if (a.residual) load8<O>(a.residual, r * a.N + n, res);
+    for (int q = 0; q < kPer; ++q) {
+      const int row = q * (64 / kLanes) + row_in;
+      const int64_t r = r0 + wr + i * 32 + row;
+      float y[8], res[8];
+      *(f32x4*)y = *(const f32x4*)(mine + at(row, c));
+      *(f32x4*)(y + 4) = *(const f32x4*)(mine + at(row, c + 1));
+      if (r >= a.R || left <= 0) continue;
+      if (a.residual) load8<O, EIGHTS>(a.residual, r * a.N + n, left, res);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = fmaf(y[e] * xs[i][q], ws[e], bias[e]);   // (a product of scales may leave fp32)
-        activate_all<O, 8>(y, a.act);
-        if (a.residual)
+      for (int e = 0; e < 8; ++e) y[e] = fmaf(y[e] * xs[i][q], ws[e], bias[e]);   // (a product of scales may leave fp32)
+      activate_all<O, 8>(y, a.act);
+      if (a.residual)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] += res[e];
-        store8<O>(a.out, r * a.N + n, y);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      const int64_t r = r0 + wr + i * 32 + col;
-      if (r >= a.R) continue;
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const float v[4] = {acc[i][j][g * 4], acc[i][j][g * 4 + 1], acc[i][j][g * 4 + 2],
-                              acc[i][j][g * 4 + 3]};
-          finish4(a, r, n0 + wn + j * 32 + g * 8 + half * 4, v);
-        }
+        for (int e = 0; e < 8; ++e) y[e] += res[e];
+      store8<O, EIGHTS>(a.out, r * a.N + n, left, y);
     }
   }
 }
@@ -618,21 +650,18 @@ hipError_t run_tile(const LinearArgs& a, hipStream_t stream) {
   const uint32_t all = tiles_r * tiles_n, per = (all + 7) / 8;
   const TileMap map{tiles_r, tiles_n, all, per};
   const uint32_t grid = 8 * per;
-  // rows that start on 16 bytes, of x and w, and of all that the epilogue touches
+  // rows of x and w that start on 16 bytes
   const bool direct = (int64_t)a.K * T::kBytes % 16 == 0 && ((uintptr_t)a.x | (uintptr_t)a.w) % 16 == 0;
-  const uintptr_t any = (uintptr_t)a.out | (uintptr_t)a.bias | (uintptr_t)a.residual | (uintptr_t)a.w_scale;
-  const bool vec = a.N % 8 == 0 && any % 16 == 0;
   const auto go = [&](auto kernel) {
     return launch_in_parts(grid, [&](uint32_t first, uint32_t count) {
       kernel<<<count, kThreads, 0, stream>>>(a, map, first);
     });
   };
-  if (direct) {
-    if (vec) return go(linear_tile_kernel<T, O, WR, WN, RT, NT, STAGES, true, true>);
-    return go(linear_tile_kernel<T, O, WR, WN, RT, NT, STAGES, false, true>);
-  }
+  const bool eights = a.N % 8 == 0;
+  if (direct && eights) return go(linear_tile_kernel<T, O, WR, WN, RT, NT, STAGES, true, true>);
+  if (direct) return go(linear_tile_kernel<T, O, WR, WN, RT, NT, STAGES, false, true>);
   if constexpr (WR * WN == 4) {
-    if (vec) return go(linear_tile_kernel<T, O, WR, WN, RT, NT, 2, true, false>);
+    if (eights) return go(linear_tile_kernel<T, O, WR, WN, RT, NT, 2, true, false>);
     return go(linear_tile_kernel<T, O, WR, WN, RT, NT, 2, false, false>);
   }
   return run_tile<T, O, 2, 2, 2, 2, 2>(a, stream);         // the held tile's registers are not free there

@@ -264,3 +264,19 @@ def test_fp32_infinities_and_largest_values(gpu, R, N, K):
         A = np.abs(s["x"].cpu().double().numpy()) @ np.abs(s["w"].cpu().double().numpy()).T
         tol = 1.13 * (K + 28) * STEP * (A + 8)
     assert (np.abs(got[fine] - want[fine]) <= tol[fine]).all()
+
+
+@pytest.mark.parametrize("K", [1, 31, 33, 65, 97, 130, 161, 193, 257, 383, 1021])
+@pytest.mark.parametrize("dtype", [F32, BF16, E4M3])
+def test_odd_rows_through_one_to_many_tiles(gpu, K, dtype):
+    """Rows off 16 bytes in tiles of 128 bytes of k, several of which are under way at once;
+    columns that end 1 to 7 into an eight, the residual updated in place."""
+    for N in (509, 516, 519):
+        out_dtype = F32 if dtype == F32 else BF16
+        _log(f"[linear] odd rows K={K} N={N} {dtype}")
+        s = _inputs(gpu, 1900, N, K, dtype, out_dtype, 31 * K + N)
+        rows = torch.arange(0, 1900, 19, device=gpu)
+        before = {**s, "residual": s["residual"].clone()}
+        got = G.grace_linear(**s, act="relu", out=s["residual"])
+        torch.cuda.synchronize()
+        _check(got, before, "relu", out_dtype, rows)
