@@ -196,7 +196,7 @@ __device__ __forceinline__ u32x4 load_chunk(const typename T::storage* row, int3
 }
 
 // ---------------------------------------------------------------------------
-// Few rows or few outputs: workgroups of 16 columns x 16 RT rows whose eight waves
+// Few rows, or few outputs of fp32: workgroups of 16 columns x 16 RT rows whose eight waves
 // share out k and add up in LDS.
 //
 // Fragments come from memory in operand layout, without LDS: a lane reads 16 (e4m3:
@@ -682,12 +682,11 @@ hipError_t run(const LinearArgs& a, hipStream_t stream) {
   };
   // Few rows: the weights' reading counts, and the few-rows kernel reads them from every
   // CU (16 x 1024 -> 4096 bf16 4.5 us against 6.4 with 64 x 64 tiles, 32 x 4096 -> 4096
-  // 14.4 against 18.8; 64 x 4096 -> 4096 21.6 against 18.8).  Few tiles of fp32, whose
-  // products take eight times as long, or of rows off 16 bytes too: eight waves share a
-  // tile there (512 x 1024 -> 512 fp32 13 us against 23).
+  // 14.4 against 18.8; 64 x 4096 -> 4096 21.6 against 18.8).  Few tiles of fp32 too, whose
+  // products take eight times as long: eight waves share a tile there (512 x 1024 -> 512
+  // 12.7 us against 22.0, 1000 x 1021 -> 509 22.6 against 26.6; in bf16 21.9 against 10.2).
   const int64_t pitch = (int64_t)a.K * T::kBytes;
-  const bool slow = T::kBytes == 4 || pitch % 16 != 0;
-  if (a.R <= 32 || (slow && tiles(64, 64) <= 128) || pitch >= (1 << 22)) {
+  if (a.R <= 32 || (T::kBytes == 4 && tiles(64, 64) <= 128) || pitch >= (1 << 22)) {
     if (a.R <= 16) return run_few<T, 1>(a, stream);
     return a.R <= 32 ? run_few<T, 2>(a, stream) : run_few<T, 4>(a, stream);
   }
